@@ -22,7 +22,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblsgd.so")
 SOURCES = ["lsgd_plan_pow2_f32.hip", "lsgd_plan_pow2_bf16.hip", "lsgd_flat_pow2_f32.hip", "lsgd_flat_pow2_bf16.hip",
            "lsgd_plan_np2.hip", "lsgd_flat_np2.hip", "lsgd_plan.hip", "lsgd_flat.hip", "lsgd_split.hip", "lsgd_stream.hip",
-           "lsgd_common.hip", "lsgd_bench.hip", "lsgd_noalloc.hip"]
+           "lsgd_common.hip", "lsgd_bench.hip", "lsgd_noalloc.hip",
+           "layers/embed.hip", "layers/quant8.hip", "layers/matmul8.hip", "layers/weight_grad8.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -55,8 +56,12 @@ def spilling_kernels(remarks: str):
     return out
 
 
+def object_of(src):
+    return os.path.join(BUILD_DIR, os.path.splitext(src)[0].replace("/", "_") + ".o")
+
+
 def _compile(src, verbose):
-    obj = os.path.join(BUILD_DIR, os.path.splitext(src)[0] + ".o")
+    obj = object_of(src)
     cmd = [HIPCC] + CFLAGS + RESOURCE_REMARKS + ["-c", os.path.join(CSRC, src), "-o", obj]
     if verbose:
         print(" ".join(cmd), file=sys.stderr)

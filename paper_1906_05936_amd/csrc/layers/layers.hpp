@@ -1,0 +1,169 @@
+// What the layer operators share: argument checks without host allocations,
+// under-aligned vector accesses, the 8-bit format.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../lsgd_host.hpp"
+#include "../lsgd_kernels.hpp"
+#include "../../../include/layers/lsgd_layers.h"
+
+#pragma clang fp contract(off)
+
+namespace lsgd {
+namespace layers {
+
+constexpr int64_t kMaxDim = 0x7fffffff;
+
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ------------------------------------------------------------------ host checks
+
+inline lsgd_status check_dtype(lsgd_dtype t, const char* what) {
+    return t == LSGD_F32 || t == LSGD_BF16 ? LSGD_OK : fail(LSGD_ERR_DTYPE, "%s=%d", what, static_cast<int>(t));
+}
+inline lsgd_status check_size(int64_t n, const char* what) {
+    return n >= 0 && n <= kMaxDim ? LSGD_OK
+                                  : fail(LSGD_ERR_SIZE, "%s=%lld outside [0, 2^31)", what, static_cast<long long>(n));
+}
+// A matrix of at most 2^46 elements: byte counts and offsets stay within 64 bits.
+inline lsgd_status check_matrix(int64_t rows, int64_t cols, const char* what) {
+    return rows == 0 || cols <= (int64_t{1} << 46) / rows
+               ? LSGD_OK
+               : fail(LSGD_ERR_SIZE, "%s of %lld x %lld elements", what, static_cast<long long>(rows),
+                      static_cast<long long>(cols));
+}
+inline lsgd_status check_buffer(const void* p, uintptr_t align, const char* what) {
+    if (!p) return fail(LSGD_ERR_NULL, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(p) & (align - 1))
+        return fail(LSGD_ERR_ALIGN, "%s is not %d-byte aligned", what, static_cast<int>(align));
+    return LSGD_OK;
+}
+inline int64_t elem_size(lsgd_dtype t) { return t == LSGD_F32 ? 4 : 2; }
+
+// LSGD_ERR_ALIAS if one of the `written` ranges overlaps another range.
+template <int N>
+struct Ranges {
+    Range r[N];
+    int n = 0;
+    void add(const void* p, int64_t bytes, bool written, const char* what) {
+        const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+        if (bytes > 0) r[n++] = Range{b, b + static_cast<uintptr_t>(bytes), written, what};
+    }
+    lsgd_status check() const {
+        for (int i = 0; i < n; ++i) {
+            if (!r[i].written) continue;
+            for (int j = 0; j < n; ++j)
+                if (j != i && r[i].begin < r[j].end && r[j].begin < r[i].end)
+                    return fail(LSGD_ERR_ALIAS, "written buffer %s overlaps %s", r[i].what, r[j].what);
+        }
+        return LSGD_OK;
+    }
+};
+
+// 8-bit matrices: bytes from row to row, and of the whole buffers.
+__host__ __device__ inline int64_t pitch8(int64_t cols) { return ceil_div(cols, 128) * 128; }
+__host__ __device__ inline int64_t scale_pitch8(int64_t cols) { return ceil_div(ceil_div(cols, 128), 4) * 4; }
+inline int64_t codes_bytes(int64_t rows, int64_t cols) { return rows * pitch8(cols); }
+inline int64_t scales_bytes(int64_t rows, int64_t cols, int64_t block) {
+    return ceil_div(rows, block) * scale_pitch8(cols);
+}
+
+#define LSGD_TRY(expr)                                 \
+    do {                                               \
+        const lsgd_status st_ = (expr);                \
+        if (st_ != LSGD_OK) return st_;                \
+    } while (0)
+
+
+// ------------------------------------------------------------------ device side
+
+// Rows of an odd length start anywhere: these types carry the alignment of one
+// element, and gfx950 loads and stores them with one 128-bit instruction.
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_u2 __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ float bf16_to_f32(uint32_t h) { return __builtin_bit_cast(float, h << 16); }
+
+// Nearest-even; a NaN stays one (quiet).
+__device__ __forceinline__ uint32_t f32_to_bf16(float f) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
+    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+}
+
+// Elements [0, k) of the 8 at p (k in [0, 8]; those behind stay 0).
+__device__ __forceinline__ void load8(const float* p, int k, float (&x)[8]) {
+    if (k >= 8) {
+        const f32x4_u a = *reinterpret_cast<const f32x4_u*>(p), b = *reinterpret_cast<const f32x4_u*>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < k ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int k, float (&x)[8]) {
+    if (k >= 8) {
+        const u32x4_u2 a = *reinterpret_cast<const u32x4_u2*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            x[2 * i] = bf16_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < k ? bf16_to_f32(p[i]) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store8(float* p, int k, const float (&x)[8]) {
+    if (k >= 8) {
+        *reinterpret_cast<f32x4_u*>(p) = f32x4_u{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4_u*>(p + 4) = f32x4_u{x[4], x[5], x[6], x[7]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < k) p[i] = x[i];
+    }
+}
+__device__ __forceinline__ void store8(uint16_t* p, int k, const float (&x)[8]) {
+    if (k >= 8) {
+        u32x4_u2 a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = f32_to_bf16(x[2 * i]) | f32_to_bf16(x[2 * i + 1]) << 16;
+        *reinterpret_cast<u32x4_u2*>(p) = a;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < k) p[i] = static_cast<uint16_t>(f32_to_bf16(x[i]));
+    }
+}
+
+// |x| where x is finite, else 0.
+__device__ __forceinline__ float finite_abs(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+    return u < 0x7f800000u ? __builtin_bit_cast(float, u) : 0.0f;
+}
+
+// The scale byte of a block whose largest finite magnitude is `a`: exponent e
+// + 127 with the smallest e in [-126, 127] for which a <= 448 * 2^e = 1.75 *
+// 2^(e+8). For a = 1.f * 2^E that is E - 8, one more where 1.f > 1.75. A
+// subnormal a (E field 0) lies far below 448 * 2^-126, the least scale's range.
+__device__ __forceinline__ uint32_t scale_byte(float a) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, a);
+    if (u == 0) return 127u;
+    const int e = static_cast<int>(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return static_cast<uint32_t>(e < 1 ? 1 : e);
+}
+// 2^-(e) for the byte e + 127 in [1, 247]: exact, normal.
+__device__ __forceinline__ float inverse_scale(uint32_t byte) {
+    return __builtin_bit_cast(float, (254u - byte) << 23);
+}
+
+// Four codes (nearest-even; every |x| <= 448, or NaN or infinity, which become NaN).
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+
+}  // namespace layers
+}  // namespace lsgd

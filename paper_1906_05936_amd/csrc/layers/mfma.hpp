@@ -1,0 +1,129 @@
+// Matrix instructions and what feeds them, for the 8-bit products.
+#pragma once
+
+#include <utility>
+
+#include "layers.hpp"
+
+namespace lsgd {
+namespace layers {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2_u2 __attribute__((ext_vector_type(2), aligned(2)));
+
+template <typename F, int... I>
+__device__ __forceinline__ void unrolled_impl(const F& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+// f(0), ..., f(N - 1), each with its index a compile-time constant.
+template <int N, typename F>
+__device__ __forceinline__ void unrolled(const F& f) {
+    unrolled_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// 16 bytes per lane from global memory into LDS: lane l's go to lds + 16 l
+// (lds the same in every lane).
+__device__ __forceinline__ void load_lds16(const void* global, void* lds) {
+    __builtin_amdgcn_global_load_lds((const LSGD_GLOBAL void*)global, (__attribute__((address_space(3))) void*)lds, 16,
+                                     0, 0);
+}
+
+// The workgroup's loads into LDS issued so far have arrived, and all its waves
+// are past their earlier LDS reads.
+__device__ __forceinline__ void loads_done() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// 32 codes of one row: a lane's part of 128 columns.
+union Codes32 {
+    u32x4 half[2];
+    i32x8 all;
+    uint32_t word[8];
+};
+
+// The 4 codes of a word times 2^(byte - 127), as bfloat16: exact unless below
+// 2^-126 or beyond its range.
+__device__ __forceinline__ u32x2 widen4(uint32_t codes, float scale) {
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
+    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
+    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// acc + x y^T over 128 columns of 16 rows each; word `U`'s byte of a lane's
+// scale word is that of its row. Which columns a lane holds does not matter, as
+// long as both sides hold the same ones.
+template <bool Exact>
+struct Product;
+
+// On the codes: the instruction multiplies by the scales.
+template <>
+struct Product<false> {
+    using Fragment = i32x8;
+    template <int U>
+    static __device__ __forceinline__ Fragment prepare(const Codes32& c, uint32_t) {
+        return c.all;
+    }
+    template <int U>
+    static __device__ __forceinline__ f32x4 multiply(const Fragment& x, uint32_t sx, const Fragment& y, uint32_t sy,
+                                                     f32x4 acc) {
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 0, 0, U, sx, U, sy);
+    }
+};
+
+// On bfloat16: each product exact, binary32 sums.
+template <>
+struct Product<true> {
+    struct Fragment {
+        bf16x8 part[4];
+    };
+    template <int U>
+    static __device__ __forceinline__ Fragment prepare(const Codes32& c, uint32_t scales) {
+        const float s = scale_value(scales >> (8 * U) & 0xffu);
+        Fragment f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32x2 a = widen4(c.word[2 * i], s), b = widen4(c.word[2 * i + 1], s);
+            f.part[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+        }
+        return f;
+    }
+    template <int U>
+    static __device__ __forceinline__ f32x4 multiply(const Fragment& x, uint32_t, const Fragment& y, uint32_t,
+                                                     f32x4 acc) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.part[i], y.part[i], acc, 0, 0, 0);
+        return acc;
+    }
+};
+
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ float value_of(uint16_t x) { return bf16_to_f32(x); }
+
+// The first k (1 to 4) of four neighbouring outputs.
+__device__ __forceinline__ void store4(float* p, int k, f32x4 v) {
+    if (k == 4) {
+        *reinterpret_cast<f32x4_u*>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < k) p[i] = v[i];
+    }
+}
+__device__ __forceinline__ void store4(uint16_t* p, int k, f32x4 v) {
+    if (k == 4) {
+        *reinterpret_cast<u32x2_u2*>(p) = u32x2_u2{f32_to_bf16(v[0]) | f32_to_bf16(v[1]) << 16,
+                                                   f32_to_bf16(v[2]) | f32_to_bf16(v[3]) << 16};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < k) p[i] = static_cast<uint16_t>(f32_to_bf16(v[i]));
+    }
+}
+
+}  // namespace layers
+}  // namespace lsgd

@@ -1,0 +1,232 @@
+// Activations and parameters in 8 bits (lsgd_layers.h): codes, and a
+// power-of-two scale for each block.
+#include "layers.hpp"
+
+namespace lsgd {
+namespace layers {
+namespace {
+
+// Block 1. A wave takes 512 columns of a row, a lane 8 of them: 16 lanes hold a
+// block of 128, whose largest magnitude goes round by lane exchanges; the four
+// scales leave as one word. Bound by the bytes of x read and codes written.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict__ x, int64_t cols, int64_t pitch,
+                                                            int64_t spitch, uint32_t groups, int64_t items,
+                                                            uint8_t* __restrict__ codes,
+                                                            uint8_t* __restrict__ scales) {
+    const uint32_t lane = threadIdx.x & 63;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6); item < items;
+         item += static_cast<int64_t>(gridDim.x) * (kBlock / 64)) {
+        const int64_t r = item / groups, c = (item % groups) * 512 + lane * 8;
+        const int k = static_cast<int>(max(static_cast<int64_t>(0), min(cols - c, static_cast<int64_t>(8))));
+        float v[8];
+        load8(x + r * cols + c, k, v);
+        float a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a = fmaxf(a, finite_abs(v[i]));
+#pragma unroll
+        for (int d = 1; d < 16; d *= 2) a = fmaxf(a, __shfl_xor(a, d));
+        const uint32_t byte = scale_byte(a);
+        const float inv = inverse_scale(byte);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= inv;
+        if (c < pitch)
+            *reinterpret_cast<u32x2*>(codes + r * pitch + c) =
+                u32x2{codes4(v[0], v[1], v[2], v[3]), codes4(v[4], v[5], v[6], v[7])};
+        const uint32_t word = __shfl(byte, 0) | __shfl(byte, 16) << 8 | __shfl(byte, 32) << 16 | __shfl(byte, 48) << 24;
+        if (lane == 0) *reinterpret_cast<uint32_t*>(scales + r * spitch + (item % groups) * 4) = word;
+    }
+}
+
+// Block 128. A workgroup holds a tile of 128 x 128 parameters in registers (a
+// lane: four times 4 rows by 4 columns), agrees on its largest magnitude, and
+// brings the codes into LDS as they are and transposed, from where every copy
+// is written in rows of 128 bytes. The transpose of each 4 x 4 happens in
+// registers. Bound by the parameters read and the copies written; up to
+// kCopies copies a launch keep their pointers in the kernel's arguments.
+constexpr int kCopies = 32;
+constexpr int kRowWords = 33;    // LDS words per row of 128 codes: rows start in different banks
+
+struct Copies {
+    uint8_t* codes[kCopies];
+    uint8_t* scales[kCopies];
+};
+
+__device__ __forceinline__ void put_tile(const uint32_t (&tile)[128][kRowWords], uint32_t byte, const Copies& to,
+                                         int n, int64_t rows, int64_t cols, int64_t r0, int64_t c0) {
+    const int64_t pitch = pitch8(cols), spitch = scale_pitch8(cols);
+    const int64_t blocks = pitch / 128, cb = c0 / 128;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 32 + threadIdx.x / 8, w = threadIdx.x % 8 * 4;
+        if (r0 + row < rows) {
+            const u32x4 v{tile[row][w], tile[row][w + 1], tile[row][w + 2], tile[row][w + 3]};
+            for (int k = 0; k < n; ++k)
+                *reinterpret_cast<u32x4*>(to.codes[k] + (r0 + row) * pitch + c0 + w * 4) = v;
+        }
+    }
+    // the scale, and behind the last block of columns the row's padding
+    const int64_t end = cb == blocks - 1 ? spitch : cb + 1;
+    for (int k = threadIdx.x; k < n; k += kBlock)
+        for (int64_t s = cb; s < end; ++s)
+            to.scales[k][r0 / 128 * spitch + s] = static_cast<uint8_t>(s == cb ? byte : 127u);
+}
+
+__global__ __launch_bounds__(kBlock) void quant_blocks_kernel(const float* __restrict__ p, int64_t rows, int64_t cols,
+                                                              Copies plain, int n_plain, Copies transposed,
+                                                              int n_transposed) {
+    __shared__ uint32_t tile[128][kRowWords];
+    __shared__ float wave_max[kBlock / 64];
+    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 128, r0 = static_cast<int64_t>(blockIdx.y) * 128;
+    const int tr = threadIdx.x / 32 * 4, tc = threadIdx.x % 32 * 4;
+    const int k = static_cast<int>(max(static_cast<int64_t>(0), min(cols - c0 - tc, static_cast<int64_t>(4))));
+    float v[4][4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int64_t r = r0 + a * 32 + tr + b;
+            const float* q = p + r * cols + c0 + tc;
+            const int kk = r < rows ? k : 0;
+            if (kk == 4) {
+                const f32x4_u x = *reinterpret_cast<const f32x4_u*>(q);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[a][b][i] = x[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[a][b][i] = i < kk ? q[i] : 0.0f;
+            }
+        }
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) m = fmaxf(m, finite_abs((&v[0][0][0])[i]));
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kBlock / 64; ++i) m = fmaxf(m, wave_max[i]);
+    const uint32_t byte = scale_byte(m);
+    const float inv = inverse_scale(byte);
+    uint32_t q[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+            q[a][b] = codes4(v[a][b][0] * inv, v[a][b][1] * inv, v[a][b][2] * inv, v[a][b][3] * inv);
+    if (n_plain > 0) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) tile[a * 32 + tr + b][tc / 4] = q[a][b];
+        __syncthreads();
+        put_tile(tile, byte, plain, n_plain, rows, cols, r0, c0);
+        __syncthreads();
+    }
+    if (n_transposed > 0) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            // bytes of (row b, column j) -> (column j, row b)
+            const uint32_t x0 = __builtin_amdgcn_perm(q[a][1], q[a][0], 0x05010400u);
+            const uint32_t x1 = __builtin_amdgcn_perm(q[a][1], q[a][0], 0x07030602u);
+            const uint32_t y0 = __builtin_amdgcn_perm(q[a][3], q[a][2], 0x05010400u);
+            const uint32_t y1 = __builtin_amdgcn_perm(q[a][3], q[a][2], 0x07030602u);
+            const int w = (a * 32 + tr) / 4;
+            tile[tc][w] = __builtin_amdgcn_perm(y0, x0, 0x05040100u);
+            tile[tc + 1][w] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);
+            tile[tc + 2][w] = __builtin_amdgcn_perm(y1, x1, 0x05040100u);
+            tile[tc + 3][w] = __builtin_amdgcn_perm(y1, x1, 0x07060302u);
+        }
+        __syncthreads();
+        put_tile(tile, byte, transposed, n_transposed, cols, rows, c0, r0);
+    }
+}
+
+}  // namespace
+}  // namespace layers
+}  // namespace lsgd
+
+using namespace lsgd;
+using namespace lsgd::layers;
+
+extern "C" {
+
+LSGD_API int64_t lsgd_pitch8(int64_t cols) { return pitch8(cols); }
+LSGD_API int64_t lsgd_scale_pitch8(int64_t cols) { return scale_pitch8(cols); }
+
+LSGD_API lsgd_status lsgd_quant8(const void* x, lsgd_dtype xdt, int64_t rows, int64_t cols, void* codes, void* scales,
+                                 void* stream) {
+    LSGD_TRY(check_dtype(xdt, "x dtype"));
+    LSGD_TRY(check_size(rows, "rows"));
+    LSGD_TRY(check_size(cols, "cols"));
+    LSGD_TRY(check_matrix(rows, cols, "x"));
+    if (rows == 0 || cols == 0) return LSGD_OK;
+    LSGD_TRY(check_buffer(x, 16, "x"));
+    LSGD_TRY(check_buffer(codes, 16, "codes"));
+    LSGD_TRY(check_buffer(scales, 16, "scales"));
+    Ranges<3> ranges;
+    ranges.add(x, rows * cols * elem_size(xdt), false, "x");
+    ranges.add(codes, codes_bytes(rows, cols), true, "codes");
+    ranges.add(scales, scales_bytes(rows, cols, 1), true, "scales");
+    LSGD_TRY(ranges.check());
+    const int64_t groups = ceil_div(cols, 512), items = rows * groups;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(kMaxGridBlocks, ceil_div(items, kBlock / 64))));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (xdt == LSGD_F32)
+        hipLaunchKernelGGL((quant_rows_kernel<float>), grid, dim3(kBlock), 0, s, static_cast<const float*>(x), cols,
+                           pitch8(cols), scale_pitch8(cols), static_cast<uint32_t>(groups), items,
+                           static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+    else
+        hipLaunchKernelGGL((quant_rows_kernel<uint16_t>), grid, dim3(kBlock), 0, s, static_cast<const uint16_t*>(x),
+                           cols, pitch8(cols), scale_pitch8(cols), static_cast<uint32_t>(groups), items,
+                           static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
+    return check_launch("lsgd_quant8");
+}
+
+LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t cols, void* const* codes,
+                                    void* const* scales, int32_t n_replicas, void* const* codes_t,
+                                    void* const* scales_t, int32_t n_transposed, void* stream) {
+    if (n_replicas < 0 || n_replicas > LSGD_MAX_REPLICAS || n_transposed < 0 || n_transposed > LSGD_MAX_REPLICAS)
+        return fail(LSGD_ERR_SIZE, "n_replicas=%d or n_transposed=%d outside [0, %d]", n_replicas, n_transposed,
+                    LSGD_MAX_REPLICAS);
+    LSGD_TRY(check_size(rows, "rows"));
+    LSGD_TRY(check_size(cols, "cols"));
+    LSGD_TRY(check_matrix(rows, cols, "params"));
+    if (ceil_div(rows, 128) > 65535)
+        return fail(LSGD_ERR_SIZE, "rows=%lld above 65535 * 128", static_cast<long long>(rows));
+    if (rows == 0 || cols == 0 || n_replicas + n_transposed == 0) return LSGD_OK;
+    LSGD_TRY(check_buffer(params, 16, "params"));
+    if ((n_replicas && (!codes || !scales)) || (n_transposed && (!codes_t || !scales_t)))
+        return fail(LSGD_ERR_NULL, "an array of copies is NULL");
+    Ranges<4 * LSGD_MAX_REPLICAS + 1> ranges;
+    ranges.add(params, rows * cols * 4, false, "params");
+    for (int32_t i = 0; i < n_replicas; ++i) {
+        LSGD_TRY(check_buffer(codes[i], 16, "a replica's codes"));
+        LSGD_TRY(check_buffer(scales[i], 16, "a replica's scales"));
+        ranges.add(codes[i], codes_bytes(rows, cols), true, "a replica's codes");
+        ranges.add(scales[i], scales_bytes(rows, cols, 128), true, "a replica's scales");
+    }
+    for (int32_t i = 0; i < n_transposed; ++i) {
+        LSGD_TRY(check_buffer(codes_t[i], 16, "a transposed replica's codes"));
+        LSGD_TRY(check_buffer(scales_t[i], 16, "a transposed replica's scales"));
+        ranges.add(codes_t[i], codes_bytes(cols, rows), true, "a transposed replica's codes");
+        ranges.add(scales_t[i], scales_bytes(cols, rows, 128), true, "a transposed replica's scales");
+    }
+    LSGD_TRY(ranges.check());
+    const dim3 grid(static_cast<unsigned>(ceil_div(cols, 128)), static_cast<unsigned>(ceil_div(rows, 128)));
+    for (int32_t at = 0; at < n_replicas || at < n_transposed; at += kCopies) {
+        Copies a{}, b{};
+        const int na = std::max(0, std::min(kCopies, n_replicas - at));
+        const int nb = std::max(0, std::min(kCopies, n_transposed - at));
+        for (int i = 0; i < na; ++i)
+            a.codes[i] = static_cast<uint8_t*>(codes[at + i]), a.scales[i] = static_cast<uint8_t*>(scales[at + i]);
+        for (int i = 0; i < nb; ++i)
+            b.codes[i] = static_cast<uint8_t*>(codes_t[at + i]), b.scales[i] = static_cast<uint8_t*>(scales_t[at + i]);
+        hipLaunchKernelGGL(quant_blocks_kernel, grid, dim3(kBlock), 0, static_cast<hipStream_t>(stream), params, rows,
+                           cols, a, na, b, nb);
+        LSGD_TRY(check_launch("lsgd_copy_out8"));
+    }
+    return LSGD_OK;
+}
+
+}  // extern "C"
