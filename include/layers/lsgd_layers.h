@@ -124,7 +124,7 @@ LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t c
  * The product of two 8-bit matrices over their columns:
  *   out[i][j] = sum over c < k of a[i][c] * b[j][c]
  * a: m x k, b: n x k (codes and scales as above, a_block and b_block 1 or 128,
- * else LSGD_ERR_UNSUPPORTED); out: m x n of dtype odt. With activations a and
+ * else LSGD_ERR_UNSUPPORTED; k at most 2^23); out: m x n of dtype odt. With activations a and
  * parameters b: a layer's output; with an output gradient a and transposed
  * parameters b: the gradient of its input.
  * odt LSGD_F32: products exact, sums in binary32 (matrix instructions on

@@ -86,12 +86,13 @@ typedef uint32_t u32x4_u2 __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t h) { return __builtin_bit_cast(float, h << 16); }
 
-// Nearest-even; a NaN stays one (quiet).
-__device__ __forceinline__ uint32_t f32_to_bf16(float f) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+// Nearest-even (one instruction for two numbers); a NaN stays one.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t f32_to_bf16x2(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{lo, hi}), bf16x2));
 }
+__device__ __forceinline__ uint32_t f32_to_bf16(float f) { return f32_to_bf16x2(f, 0.0f) & 0xffffu; }
 
 // Elements [0, k) of the 8 at p (k in [0, 8]; those behind stay 0).
 __device__ __forceinline__ void load8(const float* p, int k, float (&x)[8]) {
@@ -129,7 +130,7 @@ __device__ __forceinline__ void store8(uint16_t* p, int k, const float (&x)[8]) 
     if (k >= 8) {
         u32x4_u2 a;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = f32_to_bf16(x[2 * i]) | f32_to_bf16(x[2 * i + 1]) << 16;
+        for (int i = 0; i < 4; ++i) a[i] = f32_to_bf16x2(x[2 * i], x[2 * i + 1]);
         *reinterpret_cast<u32x4_u2*>(p) = a;
     } else {
 #pragma unroll

@@ -18,37 +18,43 @@ struct Operand {
 // (straight into LDS, no registers) overlap. LDS rows are 128 bytes, their
 // 16-byte chunks exchanged by row % 8, so that the 8 rows of a fragment read
 // meet all banks. b is the matrix instruction's first operand: a lane then holds
-// 4 neighbouring columns of one output row.
+// 4 neighbouring columns of one output row. Offsets inside a tile are 32-bit.
 template <int TM, int TN, int WM, int WN, bool Exact, typename OT>
-__global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operand B, int64_t pitch, int64_t spitch,
-                                                               OT* __restrict__ out) {
-    constexpr int kWaves = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16;
-    __shared__ __align__(16) uint8_t lds[2][(BM + BN) * 128];
+__global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
+                                                               TileOrder order, OT* __restrict__ out) {
+    constexpr int kWaves = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, kStage = (BM + BN) * 128;
+    constexpr int kLoadsA = BM / 8 / kWaves, kLoads = (BM + BN) / 8 / kWaves;   // of 8 rows each, per wave
+    static_assert(kLoadsA * 8 * kWaves == BM && kLoads * 8 * kWaves == BM + BN, "every wave loads as many rows");
+    __shared__ __align__(16) uint8_t lds[2 * kStage];
+    uint32_t tm, tn;
+    if (!order.tile(blockIdx.x, tm, tn)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t m0 = static_cast<int64_t>(blockIdx.y) * BM, n0 = static_cast<int64_t>(blockIdx.x) * BN;
+    const int64_t m0 = static_cast<int64_t>(tm) * BM, n0 = static_cast<int64_t>(tn) * BN;
     const int wm = wave % WM * (TM * 16), wn = wave / WM * (TN * 16);
     const int steps = static_cast<int>(pitch / 128);
-
     // rows past the end repeat the last one; their outputs are not stored
-    auto fetch = [&](int stage, int step) {
-        constexpr int kLoads = (BM + BN) / 8;   // of 8 rows each
+    const uint32_t last_a = static_cast<uint32_t>(min(A.rows - m0, static_cast<int64_t>(BM))) - 1;
+    const uint32_t last_b = static_cast<uint32_t>(min(B.rows - n0, static_cast<int64_t>(BN))) - 1;
+    const uint8_t* codes_a = A.codes + m0 * pitch;
+    const uint8_t* codes_b = B.codes + n0 * pitch;
+    uint32_t from[kLoads];   // a lane's 16 bytes of the rows it loads
 #pragma unroll
-        for (int i = 0; i < kLoads / kWaves; ++i) {
-            const int first = (i * kWaves + wave) * 8;
-            const int row = first + lane / 8, chunk = (lane % 8) ^ (row % 8);
-            const bool a = first < BM;
-            const int64_t r = a ? min(m0 + row, A.rows - 1) : min(n0 + row - BM, B.rows - 1);
-            load_lds16((a ? A.codes : B.codes) + r * pitch + step * 128 + chunk * 16, &lds[stage][first * 128]);
-        }
+    for (int i = 0; i < kLoads; ++i) {
+        const uint32_t row = ((i < kLoadsA ? i : i - kLoadsA) * kWaves + wave) * 8 + lane / 8;
+        from[i] = min(row, i < kLoadsA ? last_a : last_b) * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+    }
+    auto fetch = [&](uint8_t* stage) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            load_lds16((i < kLoadsA ? codes_a : codes_b) + from[i], stage + (i * kWaves + wave) * 1024);
+        codes_a += 128;
+        codes_b += 128;
     };
-    const uint8_t* sa[TM];
-    const uint8_t* sb[TN];
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-        sa[i] = A.scales + (min(m0 + wm + i * 16 + lane % 16, A.rows - 1) >> A.shift) * spitch;
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-        sb[j] = B.scales + (min(n0 + wn + j * 16 + lane % 16, B.rows - 1) >> B.shift) * spitch;
+    // scale words: a row's offset from the tile's first scale row
+    const uint8_t* scales_a = A.scales + (m0 >> A.shift) * spitch;
+    const uint8_t* scales_b = B.scales + (n0 >> B.shift) * spitch;
+    const uint32_t part_a = static_cast<uint32_t>(m0) & ((1u << A.shift) - 1);
+    const uint32_t part_b = static_cast<uint32_t>(n0) & ((1u << B.shift) - 1);
 
     f32x4 acc[TM][TN];
 #pragma unroll
@@ -56,34 +62,38 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     uint32_t wa[TM], wb[TN];
-    fetch(0, 0);
+    // fragment rows: lane % 16, whose row % 8 exchanges the chunks
+    const int at = lane % 16 * 128 + ((lane / 16) ^ (lane % 8)) * 16;
+    const int at_a = wm * 128 + at, at_b = (BM + wn) * 128 + at;
+    fetch(lds);
     for (int base = 0; base < steps; base += 4) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) wa[i] = *reinterpret_cast<const uint32_t*>(sa[i] + base);
+        for (int i = 0; i < TM; ++i)
+            wa[i] = *reinterpret_cast<const uint32_t*>(
+                scales_a + ((part_a + min(static_cast<uint32_t>(wm + i * 16 + lane % 16), last_a)) >> A.shift) * spitch + base);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) wb[j] = *reinterpret_cast<const uint32_t*>(sb[j] + base);
+        for (int j = 0; j < TN; ++j)
+            wb[j] = *reinterpret_cast<const uint32_t*>(
+                scales_b + ((part_b + min(static_cast<uint32_t>(wn + j * 16 + lane % 16), last_b)) >> B.shift) * spitch + base);
         unrolled<4>([&](auto ic) {
             constexpr int u = decltype(ic)::value;
-            const int step = base + u;
-            if (step >= steps) return;
+            if (base + u >= steps) return;
             loads_done();
-            if (step + 1 < steps) fetch((u + 1) & 1, step + 1);
-            const uint8_t* t = lds[u & 1];
-            auto fragment = [&](int row) {
-                row += lane % 16;
-                const int g = lane / 16;
+            if (base + u + 1 < steps) fetch(lds + ((u + 1) & 1) * kStage);
+            const uint8_t* t = lds + (u & 1) * kStage;
+            auto fragment = [&](int off) {
                 Codes32 f;
-                f.half[0] = *reinterpret_cast<const u32x4*>(t + row * 128 + (g ^ (row % 8)) * 16);
-                f.half[1] = *reinterpret_cast<const u32x4*>(t + row * 128 + ((g + 4) ^ (row % 8)) * 16);
+                f.half[0] = *reinterpret_cast<const u32x4*>(t + off);
+                f.half[1] = *reinterpret_cast<const u32x4*>(t + (off ^ 64));
                 return f;
             };
             using Frag = typename Product<Exact>::Fragment;
             Frag fb[TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = Product<Exact>::template prepare<u>(fragment(BM + wn + j * 16), wb[j]);
+            for (int j = 0; j < TN; ++j) fb[j] = Product<Exact>::template prepare<u>(fragment(at_b + j * 2048), wb[j]);
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const Frag fa = Product<Exact>::template prepare<u>(fragment(wm + i * 16), wa[i]);
+                const Frag fa = Product<Exact>::template prepare<u>(fragment(at_a + i * 2048), wa[i]);
 #pragma unroll
                 for (int j = 0; j < TN; ++j)
                     acc[i][j] = Product<Exact>::template multiply<u>(fb[j], wb[j], fa, wa[i], acc[i][j]);
@@ -103,11 +113,310 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
     }
 }
 
+// The kernel for many tiles: 256 x 256 outputs in four waves of 128 x 128, one on
+// each SIMD, so that a wave's fragments (64 columns of a and b at a time, for
+// instructions of 32 x 32 x 64) are read while the products of the ones before
+// them run: both live in registers, beside the 256 of the outputs. A stage (128
+// columns of a and b) is in LDS for the fragment reads while the next one
+// arrives. A workgroup goes through several tiles, and its loads run two
+// stages ahead, across the end of a tile: the next one's first stages arrive
+// while this one's outputs leave.
+constexpr int kWideTile = 256;
+
+// The stage that a workgroup loads next: tile, place in it, addresses. The last
+// tile of a row or column of tiles lies inside the matrix too, over a part of
+// the one before it: both compute the same bits there.
+struct WideLoads {
+    static constexpr int kLoads = 8;          // of 8 rows each, per wave and operand
+    static constexpr int kStage = 2 * kWideTile * 128;
+    uint32_t row_a[4], row_b[4];              // scale rows of a wave's fragments
+    Buffer codes_a, codes_b;
+    const uint8_t *scales_a, *scales_b;
+    uint32_t stage;
+
+    static __device__ __forceinline__ int64_t origin(uint32_t tile, int64_t rows) {
+        return min(static_cast<int64_t>(tile) * kWideTile, rows - kWideTile);
+    }
+    __device__ __forceinline__ WideLoads() : codes_a(nullptr, 0), codes_b(nullptr, 0) {}
+    __device__ __forceinline__ void set(const Operand& A, const Operand& B, uint32_t tm, uint32_t tn, uint32_t pitch,
+                                        uint32_t spitch, int wave, int lane) {
+        const int64_t m0 = origin(tm, A.rows), n0 = origin(tn, B.rows);
+        codes_a = Buffer(A.codes + m0 * pitch, kWideTile * pitch);
+        codes_b = Buffer(B.codes + n0 * pitch, kWideTile * pitch);
+        scales_a = A.scales + (m0 >> A.shift) * spitch;
+        scales_b = B.scales + (n0 >> B.shift) * spitch;
+        const uint32_t part_a = static_cast<uint32_t>(m0) & ((1u << A.shift) - 1);
+        const uint32_t part_b = static_cast<uint32_t>(n0) & ((1u << B.shift) - 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            row_a[i] = ((part_a + wave % 2 * 128 + i * 32 + lane % 32) >> A.shift) * spitch;
+            row_b[i] = ((part_b + wave / 2 * 128 + i * 32 + lane % 32) >> B.shift) * spitch;
+        }
+        stage = 0;
+    }
+    // `from`: a lane's 16 bytes of the wave's first 8 rows
+    __device__ __forceinline__ void fetch(uint8_t* to, uint32_t from, uint32_t pitch, int wave) const {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            codes_a.load_lds16(from, stage * 128 + i * 32 * pitch, to + (i * 4 + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            codes_b.load_lds16(from, stage * 128 + i * 32 * pitch, to + (kWideTile / 8 + i * 4 + wave) * 1024);
+    }
+    __device__ __forceinline__ void fetch_scales(uint32_t (&a)[4], uint32_t (&b)[4]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = scales_a[row_a[i] + stage], b[i] = scales_b[row_b[i] + stage];
+    }
+};
+
+__global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
+                                                           TileOrder order, uint16_t* __restrict__ out) {
+    constexpr int kStage = WideLoads::kStage;
+    __shared__ __align__(16) uint8_t lds[2 * kStage + 4 * 8192];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % 2 * 128, wn = wave / 2 * 128;
+    const uint32_t stages = pitch / 128;
+    uint32_t tm, tn, next_tm, next_tn, block = blockIdx.x;
+    if (!order.tile(block, tm, tn)) return;
+    const uint32_t from = (wave * 8 + lane / 8) * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+    WideLoads loads;
+    loads.set(A, B, tm, tn, pitch, spitch, wave, lane);
+    uint32_t sa[4], sb[4], next_sa[4], next_sb[4];
+    struct Fragments {
+        Codes32 a[4], b[4];
+    } even, odd;   // columns [0, 64) and [64, 128) of a stage
+    // a lane reads chunks 4 h + lane / 32 and the second behind it of row lane % 32
+    const uint32_t at = lane % 32 * 128 + ((lane / 32) ^ (lane % 8)) * 16;
+    auto read = [&](Fragments& f, uint32_t stage, int h) {
+        const uint8_t* x = lds + stage + (at ^ (h * 64));
+        const uint8_t* y = lds + stage + (at ^ (h * 64 + 32));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f.b[i].half[0] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
+            f.b[i].half[1] = *reinterpret_cast<const u32x4*>(y + (kWideTile + wn + i * 32) * 128);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f.a[i].half[0] = *reinterpret_cast<const u32x4*>(x + (wm + i * 32) * 128);
+            f.a[i].half[1] = *reinterpret_cast<const u32x4*>(y + (wm + i * 32) * 128);
+        }
+    };
+    loads.fetch_scales(sa, sb);
+    loads.fetch(lds, from, pitch, wave);
+    loads_done();
+    loads.stage = 1;
+    loads.fetch_scales(next_sa, next_sb);
+    loads.fetch(lds + kStage, from, pitch, wave);
+    read(even, 0, 0);
+    uint32_t here = 0;
+    for (;;) {
+        f32x16 acc[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+        auto multiply = [&](const Fragments& f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j].all, f.a[i].all, acc[i][j], 0, 0, 0,
+                                                                               sb[j], 0, sa[i]);
+        };
+        block += gridDim.x;
+        const bool more = order.tile(block, next_tm, next_tn);
+#pragma unroll 1
+        for (int last_two = 0; last_two < 2; ++last_two) {
+            // while this tile's last two stages are multiplied, the next one's first
+            // two arrive (behind the last tile its own again, which nothing reads)
+            if (last_two) {
+                if (more) loads.set(A, B, next_tm, next_tn, pitch, spitch, wave, lane);
+                loads.stage = ~0u;
+            }
+#pragma unroll 1
+            for (uint32_t t = last_two ? stages - 2 : 0; t < (last_two ? stages : stages - 2); ++t) {
+                read(odd, here, 1);
+                multiply(even);
+                interleave_reads<16>();
+                loads_done();   // this stage is in every wave's registers, and the next has arrived
+                read(even, here ^ kStage, 0);
+                multiply(odd);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sa[i] = next_sa[i], sb[i] = next_sb[i];
+                ++loads.stage;
+                loads.fetch_scales(next_sa, next_sb);
+                loads.fetch(lds + here, from, pitch, wave);
+                interleave_reads<16>();
+                here ^= kStage;
+            }
+        }
+        // 32 rows of the wave's outputs at a time pass through LDS (16-byte chunks
+        // exchanged by row), so that rows leave in runs of 256 bytes
+        uint32_t l = lane;
+        asm volatile("" : "+v"(l));   // the addresses below are not worth registers during the products
+        uint8_t* o = reinterpret_cast<uint8_t*>(out + (WideLoads::origin(tm, A.rows) + wm) * B.rows +
+                                                WideLoads::origin(tn, B.rows) + wn);
+        const uint32_t row_bytes = static_cast<uint32_t>(B.rows) * 2, lane_at = l / 16 * row_bytes + l % 16 * 16;
+        uint8_t* mine = lds + 2 * kStage + wave * 8192;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                asm volatile("" : "+a"(acc[i][j]));   // read from its accumulation registers here, not earlier
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    *reinterpret_cast<u32x2*>(mine + l % 32 * 256 + ((j * 4 + r) ^ (l % 16)) * 16 + l / 32 * 8) =
+                        u32x2{f32_to_bf16x2(acc[i][j][r * 4], acc[i][j][r * 4 + 1]),
+                              f32_to_bf16x2(acc[i][j][r * 4 + 2], acc[i][j][r * 4 + 3])};
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t row = q * 4 + l / 16;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 256 + ((l % 16) ^ (row % 16)) * 16);
+                *reinterpret_cast<u32x4_u2*>(o + lane_at) = u32x4_u2{v[0], v[1], v[2], v[3]};
+                o += 4 * static_cast<uint64_t>(row_bytes);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!more) break;
+        tm = next_tm;
+        tn = next_tn;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load into LDS outlives the workgroup
+}
+
+// The kernel for few tiles: a workgroup's W waves share one small tile of outputs
+// and divide its columns of a and b, so that a wave has K / (128 W) stages to
+// go through instead of K / 128. Each wave loads its stages into a ring of
+// D slots of LDS that are its own (in rows of 128 bytes, as the larger kernels
+// do; loads straight into registers, 64 bytes of a row each, were slower by half),
+// so nothing waits for another wave until the sums meet in LDS, added in wave
+// order.
+template <int TM, int TN, int W, int D, bool Exact, typename OT>
+__global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
+                                                                TileOrder order, OT* __restrict__ out) {
+    constexpr int kSlot = (TM + TN) * 2048, kLoads = (TM + TN) * 2;   // loads of 8 rows each
+    constexpr int kRing = W * D * kSlot, kSums = W * TM * TN * 1024;
+    __shared__ __align__(16) uint8_t lds[kRing > kSums ? kRing : kSums];
+    uint32_t tm, tn;
+    if (!order.tile(blockIdx.x, tm, tn)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t m0 = static_cast<int64_t>(tm) * (TM * 16), n0 = static_cast<int64_t>(tn) * (TN * 16);
+    const uint32_t stages = pitch / 128;
+    // rows past the end repeat the last one; their outputs are not stored
+    const uint8_t* from[kLoads];
+    const uint8_t *sa[TM], *sb[TN];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const bool a = i < TM * 2;
+        const int64_t r = a ? min(m0 + i * 8 + lane / 8, A.rows - 1) : min(n0 + (i - TM * 2) * 8 + lane / 8, B.rows - 1);
+        from[i] = (a ? A.codes : B.codes) + r * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = A.scales + (min(m0 + i * 16 + lane % 16, A.rows - 1) >> A.shift) * spitch;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = B.scales + (min(n0 + j * 16 + lane % 16, B.rows - 1) >> B.shift) * spitch;
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    uint8_t* ring = lds + wave * (D * kSlot);
+    uint32_t wa[D][TM], wb[D][TN];
+    const uint32_t each = (stages + W - 1) / W, begin = wave * each, end = min(begin + each, stages);
+    if (begin < end) {
+        // stages past the end repeat the last one, into slots that nothing reads any more
+        auto fetch = [&](uint32_t s, int d) {
+            s = min(s, end - 1);
+#pragma unroll
+            for (int i = 0; i < TM; ++i) wa[d][i] = sa[i][s];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) wb[d][j] = sb[j][s];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load_lds16(from[i] + s * 128, ring + d * kSlot + i * 1024);
+        };
+        unrolled<D>([&](auto d) { fetch(begin + decltype(d)::value, decltype(d)::value); });
+        const int at = lane % 16 * 128 + ((lane / 16) ^ (lane % 8)) * 16;
+        for (uint32_t base = begin; base < end; base += D)
+            unrolled<D>([&](auto dc) {
+                constexpr int d = decltype(dc)::value;
+                if (base + d >= end) return;
+                // all but the D - 1 stages behind this one have arrived
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * kLoads) : "memory");
+                auto fragment = [&](int off) {
+                    Codes32 f;
+                    f.half[0] = *reinterpret_cast<const u32x4*>(ring + d * kSlot + off);
+                    f.half[1] = *reinterpret_cast<const u32x4*>(ring + d * kSlot + (off ^ 64));
+                    return f;
+                };
+                using Frag = typename Product<Exact>::Fragment;
+                Codes32 ra[TM], rb[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) rb[j] = fragment((TM + j) * 2048 + at);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) ra[i] = fragment(i * 2048 + at);
+                uint32_t va[TM], vb[TN];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) va[i] = wa[d][i];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) vb[j] = wb[d][j];
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the slot is loaded again
+                fetch(base + d + D, d);
+                Frag fb[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[j] = Product<Exact>::template prepare<0>(rb[j], vb[j]);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) {
+                    const Frag fa = Product<Exact>::template prepare<0>(ra[i], va[i]);
+#pragma unroll
+                    for (int j = 0; j < TN; ++j)
+                        acc[i][j] = Product<Exact>::template multiply<0>(fb[j], vb[j], fa, va[i], acc[i][j]);
+                }
+            });
+    }
+    loads_done();   // the rings are free
+    f32x4* sums = reinterpret_cast<f32x4*>(lds);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sums[(wave * TM * TN + i * TN + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int q = wave; q < TM * TN; q += W) {
+        f32x4 v = sums[q * 64 + lane];
+        for (uint32_t w = 1; w < W && w * each < stages; ++w) v += sums[(w * TM * TN + q) * 64 + lane];
+        const int64_t m = m0 + q / TN * 16 + lane % 16, n = n0 + q % TN * 16 + lane / 16 * 4, left = B.rows - n;
+        if (m < A.rows && left > 0) store4(out + m * B.rows + n, static_cast<int>(min(left, static_cast<int64_t>(4))), v);
+    }
+}
+
 template <typename OT>
 __global__ __launch_bounds__(kBlock) void zero_kernel(OT* __restrict__ out, int64_t n) {
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < n;
          i += static_cast<int64_t>(gridDim.x) * kBlock)
         out[i] = 0;
+}
+
+template <int TM, int TN, int WM, int WN, bool Exact, typename OT>
+lsgd_status launch_tiles(const Operand& a, const Operand& b, int64_t k, void* out, hipStream_t s) {
+    const TileOrder order(ceil_div(a.rows, WM * TM * 16), ceil_div(b.rows, WN * TN * 16));
+    if (order.blocks() > kMaxGridBlocks) return fail(LSGD_ERR_SIZE, "%lld tiles", static_cast<long long>(order.blocks()));
+    hipLaunchKernelGGL((matmul8_kernel<TM, TN, WM, WN, Exact, OT>), dim3(static_cast<unsigned>(order.blocks())),
+                       dim3(WM * WN * 64), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
+                       static_cast<uint32_t>(scale_pitch8(k)), order, static_cast<OT*>(out));
+    return check_launch("lsgd_matmul8");
+}
+
+template <int TM, int TN, int W, int D, bool Exact, typename OT>
+lsgd_status launch_narrow(const Operand& a, const Operand& b, int64_t k, void* out, hipStream_t s) {
+    const TileOrder order(ceil_div(a.rows, TM * 16), ceil_div(b.rows, TN * 16));
+    hipLaunchKernelGGL((matmul8_narrow_kernel<TM, TN, W, D, Exact, OT>), dim3(static_cast<unsigned>(order.blocks())), dim3(W * 64),
+                       0, s, a, b, static_cast<uint32_t>(pitch8(k)), static_cast<uint32_t>(scale_pitch8(k)), order,
+                       static_cast<OT*>(out));
+    return check_launch("lsgd_matmul8");
 }
 
 template <bool Exact, typename OT>
@@ -118,10 +427,37 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
                            dim3(kBlock), 0, s, static_cast<OT*>(out), n);
         return check_launch("lsgd_matmul8");
     }
-    const dim3 grid(static_cast<unsigned>(ceil_div(b.rows, 128)), static_cast<unsigned>(ceil_div(a.rows, 128)));
-    hipLaunchKernelGGL((matmul8_kernel<4, 4, 2, 2, Exact, OT>), grid, dim3(256), 0, s, a, b, pitch8(k), scale_pitch8(k),
-                       static_cast<OT*>(out));
-    return check_launch("lsgd_matmul8");
+    // The smallest tile of which every compute unit gets at most one: with one
+    // round of workgroups the time is a wave's loads one after another. us, at
+    // m x n x k, 16x16 / 32x16 / 32x32 / 64x32 / 64x64 / 128x128 outputs:
+    // 16x4096x4096 5.3 / 6.2 / 7.1 / 8.0 / 10.8 / 20.9, 256x512x4096 8.2 / 7.4 / 8.4 /
+    // 11.2 / 13.5 / 25.1, 512x512x512 5.2 / 5.2 / 4.2 / 4.3 / 6.2 / 6.4, 256x2048x2048
+    // 15.8 / 15.7 / 10.0 / 6.9 / 8.9 / 13.9, 1024x1024x4096 50 / 49 / 29 / 21 / 14 / 28
+    // (about 4 of each is the call).
+    const auto fits = [&](int64_t rows, int64_t cols) {
+        return ceil_div(a.rows, rows) * ceil_div(b.rows, cols) <= device_cus();
+    };
+    if (fits(16, 16)) return launch_narrow<1, 1, 8, 2, Exact, OT>(a, b, k, out, s);
+    if (fits(32, 16)) return launch_narrow<2, 1, 8, 2, Exact, OT>(a, b, k, out, s);
+    if (fits(32, 32)) return launch_narrow<2, 2, 8, 2, Exact, OT>(a, b, k, out, s);
+    if (fits(64, 32)) return launch_narrow<4, 2, 8, 1, Exact, OT>(a, b, k, out, s);
+    if (fits(64, 64)) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
+    if constexpr (!Exact) {
+        // A round of 256 x 256 tiles takes about 1.5 times one of two 128 x 128 tiles
+        // per compute unit, which hold half of it: k = 4096, us, wide / 128 x 128:
+        // 2048x4096 55 / 39, 2560x4096 56 / 60, 4608x4096 106 / 93, 6144x4096 108 / 109,
+        // 8192x8192 228 / 286.
+        const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
+        const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
+        if (a.rows >= kWideTile && b.rows >= kWideTile && b.rows <= (1 << 24) && k > 128 &&
+            3 * ceil_div(wide.tiles(), 256) < 2 * ceil_div(tiles, 512)) {
+            hipLaunchKernelGGL(matmul8_wide_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8))), dim3(256), 0, s, a, b,
+                               static_cast<uint32_t>(pitch8(k)), static_cast<uint32_t>(scale_pitch8(k)), wide,
+                               static_cast<OT*>(out));
+            return check_launch("lsgd_matmul8");
+        }
+    }
+    return launch_tiles<4, 4, 2, 2, Exact, OT>(a, b, k, out, s);
 }
 
 }  // namespace
@@ -141,11 +477,11 @@ LSGD_API lsgd_status lsgd_matmul8(const void* a, const void* a_scales, int32_t a
         return fail(LSGD_ERR_UNSUPPORTED, "blocks of %d and %d rows; 1 or 128 are supported", a_block, b_block);
     LSGD_TRY(check_size(m, "m"));
     LSGD_TRY(check_size(n, "n"));
-    LSGD_TRY(check_size(k, "k"));
+    // 256 rows of a tile lie within 32-bit offsets
+    if (k < 0 || k > (1 << 23)) return fail(LSGD_ERR_SIZE, "k=%lld outside [0, 2^23]", static_cast<long long>(k));
     LSGD_TRY(check_matrix(m, k, "a"));
     LSGD_TRY(check_matrix(n, k, "b"));
     LSGD_TRY(check_matrix(m, n, "out"));
-    if (ceil_div(m, 128) > 65535) return fail(LSGD_ERR_SIZE, "m=%lld above 65535 * 128", static_cast<long long>(m));
     if (m == 0 || n == 0) return LSGD_OK;
     LSGD_TRY(check_buffer(out, 16, "out"));
     Ranges<5> ranges;

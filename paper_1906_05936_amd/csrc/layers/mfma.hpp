@@ -9,7 +9,7 @@ namespace lsgd {
 namespace layers {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2_u2 __attribute__((ext_vector_type(2), aligned(2)));
 
@@ -23,6 +23,28 @@ __device__ __forceinline__ void unrolled(const F& f) {
     unrolled_impl(f, std::make_integer_sequence<int, N>{});
 }
 
+// Which tile of an nm x nn grid of outputs a workgroup computes. Workgroups go
+// round the eight XCDs; each XCD takes a run of consecutive tiles, counted down
+// 8 tile rows before the next tile column, so that the 32 tiles it works on at
+// a time share 8 row blocks of one operand and 4 of the other in its L2.
+struct TileOrder {
+    static constexpr uint32_t kRows = 8;
+    uint32_t nm, nn, run;   // run: tiles of an XCD
+    __host__ TileOrder(int64_t m, int64_t n)
+        : nm(static_cast<uint32_t>(m)), nn(static_cast<uint32_t>(n)), run(static_cast<uint32_t>((m * n + 7) / 8)) {}
+    __host__ int64_t tiles() const { return static_cast<int64_t>(nm) * nn; }
+    __host__ int64_t blocks() const { return static_cast<int64_t>(run) * 8; }
+    __device__ bool tile(uint32_t block, uint32_t& tm, uint32_t& tn) const {
+        const uint32_t t = (block & 7) * run + (block >> 3);
+        if (block >> 3 >= run || t >= nm * nn) return false;
+        const uint32_t band = t / (kRows * nn), in = t - band * (kRows * nn);
+        const uint32_t rows = min(kRows, nm - band * kRows);
+        tm = band * kRows + in % rows;
+        tn = in / rows;
+        return true;
+    }
+};
+
 // 16 bytes per lane from global memory into LDS: lane l's go to lds + 16 l
 // (lds the same in every lane).
 __device__ __forceinline__ void load_lds16(const void* global, void* lds) {
@@ -30,12 +52,36 @@ __device__ __forceinline__ void load_lds16(const void* global, void* lds) {
                                      0, 0);
 }
 
+// `bytes` from p on, addressed by a lane's 32-bit offset plus a uniform one.
+struct Buffer {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Buffer(const void* p, uint32_t bytes)
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000)) {}
+    // as load_lds16
+    __device__ __forceinline__ void load_lds16(uint32_t offset, uint32_t uniform, void* lds) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, offset, uniform, 0, 0);
+    }
+};
+
+// Shapes the instructions of a stretch of code between barriers: N times a
+// matrix instruction, an LDS read and two global loads, as far as there are any.
+template <int N>
+__device__ __forceinline__ void interleave_reads() {
+    unrolled<N>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x20, 2, 0);
+    });
+}
+
 // The workgroup's loads into LDS issued so far have arrived, and all its waves
 // are past their earlier LDS reads.
 __device__ __forceinline__ void loads_done() {
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // 32 codes of one row: a lane's part of 128 columns.
@@ -116,8 +162,7 @@ __device__ __forceinline__ void store4(float* p, int k, f32x4 v) {
 }
 __device__ __forceinline__ void store4(uint16_t* p, int k, f32x4 v) {
     if (k == 4) {
-        *reinterpret_cast<u32x2_u2*>(p) = u32x2_u2{f32_to_bf16(v[0]) | f32_to_bf16(v[1]) << 16,
-                                                   f32_to_bf16(v[2]) | f32_to_bf16(v[3]) << 16};
+        *reinterpret_cast<u32x2_u2*>(p) = u32x2_u2{f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3])};
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
