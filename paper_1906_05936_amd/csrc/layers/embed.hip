@@ -57,18 +57,27 @@ void launch_lookup(const void* table, int64_t rows, int64_t dim, const void* tok
 // ---------------------------------------------------------------- gradient
 //
 // The E = n_workers * n_tokens entries (entry e: worker e / n_tokens, position
-// e % n_tokens) are sorted by token, equal tokens by entry; `first` and `last`
-// bound each row's entries in the sorted order. Then every row of the gradient
-// is written once by the wave that sums its entries; a row of many entries
-// (frequent tokens hold up to a tenth of a text) is summed in pieces first, so
-// that no wave has a long list to itself. Bound by the gradients read and the
-// table written; the sort moves a few bytes per token.
+// e % n_tokens) are sorted by token, equal tokens by entry. The sorted order is
+// cut into pieces, and a wave sums a piece's gradients run by run of equal
+// tokens. A row of no more entries than a piece has belongs to the wave in whose
+// piece it starts, which writes it at once; of a longer one every piece's part
+// goes to a slot, and a last kernel adds these. So the work is divided by
+// entries, whatever the tokens' frequencies (a wave per row took 670 us where
+// one row had a tenth of all entries). Rows without entries are written by the
+// same launch. Bound by the gradients read and the table written; the sort
+// moves a few bytes per token.
 
-constexpr int kSortTile = 2048;       // entries a workgroup of the radix sort holds
-constexpr int kDigitBits = 9;         // two passes for tables of up to 2^18 - 1 rows
+constexpr int kSortThreads = 512, kSortRounds = 8;
+constexpr int kSortTile = kSortThreads * kSortRounds;   // entries a workgroup of the radix sort holds
+constexpr int kDigitBits = 9;              // two passes for tables of up to 2^18 - 1 rows
 constexpr int kBins = 1 << kDigitBits;
-constexpr int kRankMax = 4096;        // entries that are sorted by counting smaller ones
-constexpr int kPiece = 64;            // sorted entries in a piece
+constexpr int kOwnSums = 256;              // up to so many workgroups each add up the counts before its own
+constexpr int kRankMax = 4096;             // entries that are sorted by counting smaller ones
+// Sorted entries in a piece, which a wave's lanes hold: with few entries latency
+// counts, and 16 in a row are faster (509 entries: 24 us, with 32 30, with 64 46);
+// with many, the slots' bytes (131072 entries: 432, 413, 417 us).
+constexpr int kFewPiece = 8, kManyPiece = 32, kFewAhead = 8, kManyAhead = 4;
+constexpr int64_t kMaxEntries = 1 << 28;   // grids over pieces stay within a dispatch
 
 struct Workers {
     const void* grads[kMaxWorkers];
@@ -78,8 +87,8 @@ struct Workers {
 struct Sorted {
     uint32_t* key;     // [E] row, or `rows` for tokens outside the table
     uint32_t* entry;   // [E]
-    uint32_t* first;   // [rows]
-    uint32_t* last;    // [rows]
+    uint32_t* last;    // [rows] end of the row's entries, 0 for a row without
+    uint32_t* starts;  // [pieces] whether a row of several pieces starts in it
 };
 
 template <typename I>
@@ -90,15 +99,20 @@ __device__ __forceinline__ uint32_t key_of(const Workers& w, uint32_t e, uint32_
     return v >= 0 && v < static_cast<int64_t>(rows) ? static_cast<uint32_t>(v) : rows;
 }
 
-__global__ __launch_bounds__(kBlock) void clear_bounds_kernel(uint32_t* __restrict__ p, int64_t n) {
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kBlock + threadIdx.x; i < n;
-         i += static_cast<int64_t>(gridDim.x) * kBlock)
+// p[0..n) = 0, by `count` workgroups of which this is number `block`.
+__device__ __forceinline__ void clear(uint32_t* p, uint32_t n, uint32_t block, uint32_t count) {
+    for (uint64_t i = static_cast<uint64_t>(block) * blockDim.x + threadIdx.x; i < n;
+         i += static_cast<uint64_t>(count) * blockDim.x)
         p[i] = 0;
+}
+
+__global__ __launch_bounds__(kBlock) void clear_kernel(uint32_t* __restrict__ p, uint32_t n) {
+    clear(p, n, blockIdx.x, gridDim.x);
 }
 
 // Rank of an entry = entries with a smaller key + earlier entries with the same
 // one. A workgroup ranks 64 entries, its 16 waves counting over a sixteenth of
-// all entries each; E^2 comparisons in one launch, against six for the radix
+// all entries each; E^2 comparisons in one launch, against four for the radix
 // sort (which takes over where E^2 shows).
 template <typename I>
 __global__ __launch_bounds__(1024) void rank_kernel(Workers w, uint32_t n_tokens, uint32_t E, uint32_t rows, Sorted s) {
@@ -126,13 +140,12 @@ __global__ __launch_bounds__(1024) void rank_kernel(Workers w, uint32_t n_tokens
         for (int i = 0; i < 16; ++i) lt += part[0][i][lane], eq += part[1][i][lane], before += part[2][i][lane];
         s.key[lt + before] = k;
         s.entry[lt + before] = e;
-        if (k < rows && before == 0) s.first[k] = lt, s.last[k] = lt + eq;
+        if (k < rows && before == 0) s.last[k] = lt + eq;
     }
 }
 
-// Radix sort, least significant digit first; three launches a pass: each
-// workgroup's counts per digit, their running sum over (digit, workgroup), and
-// the entries in their new places, in order.
+// Radix sort, least significant digit first; two launches a pass: each
+// workgroup's counts per digit, and the entries in their new places, in order.
 template <typename I, bool First>
 __device__ __forceinline__ uint32_t sort_key(const Workers& w, const uint32_t* key, uint32_t p, uint32_t n_tokens,
                                              uint32_t rows) {
@@ -140,81 +153,90 @@ __device__ __forceinline__ uint32_t sort_key(const Workers& w, const uint32_t* k
     return key[p];
 }
 
+// counts[block][digit]; the workgroups behind the `blocks` that count clear `last`.
 template <typename I, bool First>
-__global__ __launch_bounds__(kBlock) void digit_count_kernel(Workers w, const uint32_t* __restrict__ key,
-                                                             uint32_t n_tokens, uint32_t E, uint32_t rows, int shift,
-                                                             uint32_t* __restrict__ counts) {
+__global__ __launch_bounds__(kSortThreads) void digit_count_kernel(Workers w, const uint32_t* __restrict__ key,
+                                                                   uint32_t n_tokens, uint32_t E, uint32_t rows,
+                                                                   int shift, uint32_t blocks,
+                                                                   uint32_t* __restrict__ counts,
+                                                                   uint32_t* __restrict__ last) {
     __shared__ uint32_t c[kBins];
-    for (int i = threadIdx.x; i < kBins; i += kBlock) c[i] = 0;
+    if (blockIdx.x >= blocks) return clear(last, rows, blockIdx.x - blocks, gridDim.x - blocks);
+    for (int i = threadIdx.x; i < kBins; i += kSortThreads) c[i] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortTile / kBlock; ++i) {
-        const uint32_t p = blockIdx.x * kSortTile + i * kBlock + threadIdx.x;
+    for (int i = 0; i < kSortRounds; ++i) {
+        const uint32_t p = blockIdx.x * kSortTile + i * kSortThreads + threadIdx.x;
         if (p < E) atomicAdd(&c[sort_key<I, First>(w, key, p, n_tokens, rows) >> shift & (kBins - 1)], 1u);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < kBins; i += kBlock) counts[static_cast<size_t>(i) * gridDim.x + blockIdx.x] = c[i];
+    for (int i = threadIdx.x; i < kBins; i += kSortThreads) counts[static_cast<size_t>(blockIdx.x) * kBins + i] = c[i];
 }
 
-// counts[0..n) = sum of the counts before each; one workgroup.
-__global__ __launch_bounds__(1024) void running_sum_kernel(uint32_t* __restrict__ counts, uint32_t n) {
-    __shared__ uint32_t wave_sum[16];
-    uint32_t carry = 0;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (uint32_t base = 0; base < n; base += 4096) {
-        const uint32_t i = base + threadIdx.x * 4;
-        uint32_t v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = i + j < n ? counts[i + j] : 0;
-        const uint32_t mine = v[0] + v[1] + v[2] + v[3];
-        uint32_t sum = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t o = __shfl_up(sum, d);
-            if (lane >= static_cast<uint32_t>(d)) sum += o;
-        }
-        if (lane == 63) wave_sum[wave] = sum;
-        __syncthreads();
-        uint32_t before = carry, all = 0;
-#pragma unroll
-        for (uint32_t k = 0; k < 16; ++k) {
-            const uint32_t x = wave_sum[k];
-            before += k < wave ? x : 0;
-            all += x;
-        }
-        carry += all;
-        uint32_t at = before + sum - mine;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (i + j < n) counts[i + j] = at;
-            at += v[j];
-        }
-        __syncthreads();
+// For many workgroups: counts[b][d] = the entries of digit d in the workgroups
+// before b, totals[d] = those of all. One workgroup per 64 digits, its waves
+// adding an eighth of the workgroups each, twice.
+__global__ __launch_bounds__(512) void block_sums_kernel(uint32_t* __restrict__ counts, uint32_t blocks,
+                                                         uint32_t* __restrict__ totals) {
+    __shared__ uint32_t part[8][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
+    const uint32_t each = (blocks + 7) / 8, b0 = min(wave * each, blocks), b1 = min(b0 + each, blocks);
+    uint32_t sum = 0;
+#pragma unroll 8
+    for (uint32_t b = b0; b < b1; ++b) sum += counts[static_cast<size_t>(b) * kBins + d];
+    part[wave][lane] = sum;
+    __syncthreads();
+    uint32_t at = 0;
+    for (uint32_t v = 0; v < wave; ++v) at += part[v][lane];
+    for (uint32_t b = b0; b < b1; ++b) {
+        const uint32_t n = counts[static_cast<size_t>(b) * kBins + d];
+        counts[static_cast<size_t>(b) * kBins + d] = at;
+        at += n;
     }
+    if (wave == 7) totals[d] = at;
 }
 
 template <typename I, bool First>
-__global__ __launch_bounds__(kBlock) void digit_place_kernel(Workers w, const uint32_t* __restrict__ key,
-                                                             const uint32_t* __restrict__ entry, uint32_t n_tokens,
-                                                             uint32_t E, uint32_t rows, int shift,
-                                                             const uint32_t* __restrict__ counts,
-                                                             uint32_t* __restrict__ key_out,
-                                                             uint32_t* __restrict__ entry_out) {
-    constexpr int kWaves = kBlock / 64, kRounds = kSortTile / kBlock;
+__global__ __launch_bounds__(kSortThreads) void digit_place_kernel(Workers w, const uint32_t* __restrict__ key,
+                                                                   const uint32_t* __restrict__ entry,
+                                                                   uint32_t n_tokens, uint32_t E, uint32_t rows,
+                                                                   int shift, const uint32_t* __restrict__ counts,
+                                                                   const uint32_t* __restrict__ totals,
+                                                                   uint32_t* __restrict__ key_out,
+                                                                   uint32_t* __restrict__ entry_out) {
+    constexpr int kWaves = kSortThreads / 64;
+    static_assert(kSortThreads == kBins, "a lane adds up the counts of one digit");
     __shared__ uint32_t c[kWaves][kBins];
+    __shared__ uint32_t wave_sum[kWaves];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int i = threadIdx.x; i < kWaves * kBins; i += kBlock) (&c[0][0])[i] = 0;
+    uint32_t k[kSortRounds], e[kSortRounds], rank[kSortRounds];
+    const uint32_t p0 = blockIdx.x * kSortTile + wave * (kSortRounds * 64) + lane;
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {
+        const uint32_t p = min(p0 + r * 64, E - 1);
+        k[r] = sort_key<I, First>(w, key, p, n_tokens, rows);
+        e[r] = First ? p : entry[p];
+    }
+    // this lane's digit: its entries in the workgroups before this one, and in all
+    uint32_t before = 0, all = 0;
+    if (totals) {
+        before = counts[static_cast<size_t>(blockIdx.x) * kBins + threadIdx.x];
+        all = totals[threadIdx.x];
+    } else {
+#pragma unroll 16
+        for (uint32_t b = 0; b < gridDim.x; ++b) {
+            const uint32_t n = counts[static_cast<size_t>(b) * kBins + threadIdx.x];
+            before += b < blockIdx.x ? n : 0;
+            all += n;
+        }
+    }
+    for (int i = threadIdx.x; i < kWaves * kBins; i += kSortThreads) (&c[0][0])[i] = 0;
     __syncthreads();
     // A wave's 512 entries in order, 64 at a time: an entry's rank among its
-    // wave's entries of the same digit is the count so far plus the lanes
-    // before it.
-    uint32_t k[kRounds], rank[kRounds];
-    const uint32_t p0 = blockIdx.x * kSortTile + wave * (kRounds * 64) + lane;
+    // wave's entries of the same digit is the count so far plus the lanes before it.
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
-        const uint32_t p = p0 + r * 64;
-        const bool in = p < E;
-        k[r] = in ? sort_key<I, First>(w, key, p, n_tokens, rows) : 0;
+    for (int r = 0; r < kSortRounds; ++r) {
+        const bool in = p0 + r * 64 < E;
         const uint32_t d = k[r] >> shift & (kBins - 1);
         uint64_t same = __ballot(in);
 #pragma unroll
@@ -231,152 +253,206 @@ __global__ __launch_bounds__(kBlock) void digit_place_kernel(Workers w, const ui
         }
         __builtin_amdgcn_wave_barrier();
     }
-    __syncthreads();
-    for (int d = threadIdx.x; d < kBins; d += kBlock) {
-        uint32_t at = counts[static_cast<size_t>(d) * gridDim.x + blockIdx.x];
+    // where the digit starts: a running sum of the totals
+    uint32_t sum = all;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-            const uint32_t n = c[v][d];
-            c[v][d] = at;
-            at += n;
-        }
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_up(sum, d);
+        if (lane >= static_cast<uint32_t>(d)) sum += o;
+    }
+    if (lane == 63) wave_sum[wave] = sum;
+    __syncthreads();
+    uint32_t at = sum - all + before;
+    for (uint32_t v = 0; v < wave; ++v) at += wave_sum[v];
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+        const uint32_t n = c[v][threadIdx.x];
+        c[v][threadIdx.x] = at;
+        at += n;
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < kSortRounds; ++r) {
         const uint32_t p = p0 + r * 64;
         if (p < E) {
             const uint32_t to = c[wave][k[r] >> shift & (kBins - 1)] + rank[r];
             key_out[to] = k[r];
-            entry_out[to] = First ? p : entry[p];
+            entry_out[to] = e[r];
         }
     }
 }
 
-__global__ __launch_bounds__(kBlock) void row_bounds_kernel(Sorted s, uint32_t E, uint32_t rows) {
+__global__ __launch_bounds__(kBlock) void row_ends_kernel(Sorted s, uint32_t E, uint32_t rows) {
     const uint32_t p = blockIdx.x * kBlock + threadIdx.x;
     if (p >= E) return;
     const uint32_t k = s.key[p];
-    if (k >= rows) return;
-    if (p == 0 || s.key[p - 1] != k) s.first[k] = p;
-    if (p + 1 == E || s.key[p + 1] != k) s.last[k] = p + 1;
+    if (k < rows && (p + 1 == E || s.key[p + 1] != k)) s.last[k] = p + 1;
 }
 
-// acc += the gradients of sorted entries [p, q), columns c.. of the lane, in order.
-template <typename GT>
-__device__ __forceinline__ void sum_entries(const Workers& w, const uint32_t* entry, uint32_t p, uint32_t q,
-                                            uint32_t n_tokens, int64_t dim, int64_t c, int k, float (&acc)[8]) {
-    for (; p < q; p += 64) {
-        const uint32_t lane = threadIdx.x & 63, n = min(q - p, 64u);
-        const uint32_t e = lane < n ? entry[p + lane] : 0;
-        const uint32_t wk = e / n_tokens;
-        const uint64_t at = reinterpret_cast<uint64_t>(w.grads[wk]) +
-                            static_cast<uint64_t>(e - wk * n_tokens) * static_cast<uint64_t>(dim) * sizeof(GT);
-        const uint32_t lo = static_cast<uint32_t>(at), hi = static_cast<uint32_t>(at >> 32);
-        auto row = [&](uint32_t j) {
-            // readlane gives a signed int: its low half must not be sign-extended
-            const uint32_t l = __builtin_amdgcn_readlane(lo, j), h = __builtin_amdgcn_readlane(hi, j);
-            return reinterpret_cast<const GT*>(static_cast<uint64_t>(h) << 32 | l) + c;
-        };
-        uint32_t j = 0;
-        for (; j + 4 <= n; j += 4) {
-            float x[4][8];
+// scale * acc (+ out) into a row, from the lane's column on.
+template <typename OT>
+__device__ __forceinline__ void put_row(OT* row, int64_t col, int64_t dim, float scale, bool accumulate,
+                                        const float (&acc)[8]) {
+    float y[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) load8(row(j + u), k, x[u]);
+    for (int i = 0; i < 8; ++i) y[i] = acc[i] * scale;
+    if (accumulate) {
+        float x[8];
+        load_slab(row, col, dim, x);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] += x[u][i];
-        }
-        for (; j < n; ++j) {
-            float x[8];
-            load8(row(j), k, x);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] += x[i];
-        }
+        for (int i = 0; i < 8; ++i) y[i] += x[i];
     }
+    store_slab(row, col, dim, y);
 }
 
-// Partial sums of the rows with more than kPiece entries: a wave sums the
-// entries of one aligned piece [64 c, 64 c + 64) of the sorted order that belong
-// to the row of its first entry (slot 2c) or, if that is another, of its last
-// (slot 2c + 1). No third row of a piece has that many entries.
-template <typename GT>
-__global__ __launch_bounds__(kBlock) void piece_sums_kernel(Workers w, Sorted s, uint32_t n_tokens, uint32_t E,
-                                                            uint32_t rows, int64_t dim, uint32_t slabs,
-                                                            float* __restrict__ slots) {
-    const uint32_t lane = threadIdx.x & 63;
-    const uint64_t item = static_cast<uint64_t>(blockIdx.x) * (kBlock / 64) + (threadIdx.x >> 6);
-    const uint32_t c = static_cast<uint32_t>(item / slabs), slab = static_cast<uint32_t>(item % slabs);
-    const uint64_t p0 = static_cast<uint64_t>(c) * kPiece;
-    if (p0 >= E) return;
-    const uint32_t p = static_cast<uint32_t>(p0), q = min(p + kPiece, E);
-    const int64_t col = static_cast<int64_t>(slab) * 512 + lane * 8;
-    const int k = static_cast<int>(max(static_cast<int64_t>(0), min(dim - col, static_cast<int64_t>(8))));
-    const uint32_t k0 = __builtin_amdgcn_readfirstlane(s.key[p]), k1 = __builtin_amdgcn_readfirstlane(s.key[q - 1]);
-    for (int side = 0; side < 2; ++side) {
-        const uint32_t v = side ? k1 : k0;
-        if ((side && k1 == k0) || v >= rows) continue;
-        const uint32_t a = __builtin_amdgcn_readfirstlane(s.first[v]), b = __builtin_amdgcn_readfirstlane(s.last[v]);
-        if (b - a <= kPiece) continue;
-        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        sum_entries<GT>(w, s.entry, max(a, p), min(b, q), n_tokens, dim, col, k, acc);
-        store8(slots + (2 * static_cast<int64_t>(c) + side) * dim + col, k, acc);
-    }
-}
+// Workgroups below `piece_blocks`: a wave sums one piece, 512 columns. The
+// others write zeros into the rows without entries, kZeroRows at a time.
+constexpr uint32_t kZeroRows = 16;
 
-// Every row: its entries' sum, or that of its pieces, times scale. A workgroup
-// takes 16 rows; a wave one row's slab of 512 columns at a time.
-constexpr int kRowsPerBlock = 16;
-
-template <typename GT, typename OT>
-__global__ __launch_bounds__(kBlock) void row_sums_kernel(Workers w, Sorted s, uint32_t n_tokens, uint32_t rows,
-                                                          int64_t dim, uint32_t slabs, float scale,
-                                                          const float* __restrict__ slots, OT* __restrict__ out,
-                                                          bool accumulate) {
+template <int kPiece, typename GT, typename OT>
+__global__ __launch_bounds__(kBlock) void sum_pieces_kernel(Workers w, Sorted s, uint32_t n_tokens, uint32_t E,
+                                                            uint32_t rows, int64_t dim, uint32_t slabs, float scale,
+                                                            uint32_t piece_blocks, float* __restrict__ slots,
+                                                            OT* __restrict__ out, bool accumulate) {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (uint32_t v0 = blockIdx.x * kRowsPerBlock; v0 < rows; v0 += gridDim.x * kRowsPerBlock) {
-        const uint32_t nv = min(static_cast<uint32_t>(kRowsPerBlock), rows - v0);
-        const uint32_t mine = v0 + min(lane, nv - 1);
-        const uint32_t firsts = s.first ? s.first[mine] : 0, lasts = s.first ? s.last[mine] : 0;
-        for (uint32_t item = wave; item < nv * slabs; item += kBlock / 64) {
-            const uint32_t r = item / slabs, slab = item % slabs;
-            const uint32_t a = __builtin_amdgcn_readlane(firsts, r), b = __builtin_amdgcn_readlane(lasts, r);
-            if (accumulate && a == b) continue;
-            const int64_t col = static_cast<int64_t>(slab) * 512 + lane * 8;
-            const int k = static_cast<int>(max(static_cast<int64_t>(0), min(dim - col, static_cast<int64_t>(8))));
-            float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (b - a <= kPiece) {
-                sum_entries<GT>(w, s.entry, a, b, n_tokens, dim, col, k, acc);
-            } else {
-                // a piece's slot 2c is the row of its first entry, so only the piece
-                // in which the row starts, if not at its first entry, has it in 2c + 1
-                for (uint32_t c = a / kPiece; c <= (b - 1) / kPiece; ++c) {
-                    const bool starts = c == a / kPiece && s.key[static_cast<size_t>(c) * kPiece] != v0 + r;
-                    float x[8];
-                    load8(slots + (2 * static_cast<int64_t>(c) + starts) * dim + col, k, x);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] += x[i];
-                }
+    if (blockIdx.x >= piece_blocks) {
+        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        const uint32_t stride = (gridDim.x - piece_blocks) * kZeroRows;
+        for (uint64_t v0 = static_cast<uint64_t>(blockIdx.x - piece_blocks) * kZeroRows; v0 < rows; v0 += stride) {
+            const uint32_t n = min(kZeroRows, static_cast<uint32_t>(rows - v0));
+            const uint64_t empty = __ballot(lane < n && (E == 0 || s.last[v0 + min(lane, n - 1)] == 0));
+            for (uint32_t item = wave; item < n * slabs; item += kBlock / 64) {
+                if (empty >> (item / slabs) & 1)
+                    store_slab(out + static_cast<int64_t>(v0 + item / slabs) * dim, slab_column(item % slabs, lane), dim, zero);
             }
-            OT* o = out + static_cast<int64_t>(v0 + r) * dim + col;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] *= scale;
-            if (accumulate) {
-                float x[8];
-                load8(o, k, x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[i] += x[i];
-            }
-            store8(o, k, acc);
         }
+        return;
+    }
+    const uint32_t item = blockIdx.x * (kBlock / 64) + wave, c = item / slabs, p = c * kPiece;
+    if (p >= E) return;
+    const int64_t col = slab_column(item % slabs, lane);
+    // lanes: entries [p, p + 2 kPiece); keys past the end match none
+    constexpr uint32_t kP = kPiece;
+    const bool in = lane < 2 * kP && p + lane < E;
+    const uint32_t key = in ? s.key[p + lane] : ~0u, e = in ? s.entry[p + lane] : 0, wk = e / n_tokens;
+    const uint32_t ahead = lane < kP && p + lane >= kP ? s.key[p + lane - kP] : ~0u;   // of the kPiece entries before
+    const uint64_t at = reinterpret_cast<uint64_t>(w.grads[wk]) +
+                        static_cast<uint64_t>(e - wk * n_tokens) * static_cast<uint64_t>(dim) * sizeof(GT);
+    const uint32_t lo = static_cast<uint32_t>(at), hi = static_cast<uint32_t>(at >> 32);
+    const uint32_t n = min(kP, E - p);
+    const uint32_t k_first = __builtin_amdgcn_readlane(key, 0), k_last = __builtin_amdgcn_readlane(key, n - 1);
+    const uint32_t before = __popcll(__ballot(ahead == k_first)), with = __popcll(__ballot(key == k_first));
+    const uint32_t of_last = __popcll(__ballot(key == k_last));
+    // [from, to): the entries to add; first: they begin with a part of a longer row
+    // that began before; leaves: they end with a part of one that goes on
+    const bool first = before > 0 && before + with > kP;
+    const uint32_t from = before > 0 && !first ? with : 0;
+    const bool leaves = k_last < rows && !(k_last == k_first && before > 0) && of_last > kP;
+    const uint64_t mine = __ballot(in && key < rows);   // tokens outside the table come last
+    uint32_t to = n;
+    if (!leaves && !(k_last == k_first && before > 0))
+        to = max(n, 64 - static_cast<uint32_t>(__clzll(static_cast<long long>(__ballot(key == k_last)))));
+    to = min(to, static_cast<uint32_t>(__popcll(mine)));
+    if (item % slabs == 0 && lane == 0) s.starts[c] = leaves;
+    const uint32_t next = __shfl_down(key, 1);
+    uint64_t ends = __ballot(lane == 63 || next != key);
+    if (to > 0) ends |= 1ull << (to - 1);
+    auto row = [&](uint32_t j) {
+        // readlane gives a signed int: its low half must not be sign-extended
+        const uint32_t l = __builtin_amdgcn_readlane(lo, j), h = __builtin_amdgcn_readlane(hi, j);
+        return reinterpret_cast<const GT*>(static_cast<uint64_t>(h) << 32 | l);
+    };
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    constexpr int kAhead = kPiece == kFewPiece ? kFewAhead : kManyAhead;   // rows whose loads are in flight
+    bool slot_first = first;
+    for (uint32_t j = from; j < to; j += kAhead) {
+        float x[kAhead][8];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) load_slab_once(row(min(j + u, to - 1)), col, dim, x[u]);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (j + u >= to) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += x[u][i];
+            if (ends >> (j + u) & 1) {
+                const bool slot_last = leaves && j + u == to - 1;
+                if (slot_first || slot_last)
+                    store_slab(slots + (2 * static_cast<int64_t>(c) + (slot_first ? 0 : 1)) * dim, col, dim, acc);
+                else
+                    put_row(out + static_cast<int64_t>(__builtin_amdgcn_readlane(key, j + u)) * dim, col, dim, scale,
+                            accumulate, acc);
+                slot_first = false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+            }
+        }
+    }
+}
+
+// Rows of several pieces: a workgroup adds the slot 2c + 1 of the piece c in which
+// the row starts and the following pieces' slots 2c, divided over its waves in
+// order, then the waves' sums in order. It looks at kJoin pieces, 512 columns.
+constexpr uint32_t kJoin = 8;
+constexpr int kJoinThreads = 512;
+
+template <int kPiece, typename OT>
+__global__ __launch_bounds__(kJoinThreads) void join_pieces_kernel(Sorted s, uint32_t pieces, int64_t dim, uint32_t slabs,
+                                                             float scale, const float* __restrict__ slots,
+                                                             OT* __restrict__ out, bool accumulate) {
+    constexpr uint32_t kWaves = kJoinThreads / 64;
+    __shared__ float sums[kWaves - 1][512];
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t c0 = blockIdx.x / slabs * kJoin;
+    const int64_t col = slab_column(blockIdx.x % slabs, lane);
+    const uint32_t c_mine = c0 + lane;
+    const bool start = lane < kJoin && c_mine < pieces && s.starts[c_mine] != 0;
+    const uint32_t v_mine = start ? s.key[static_cast<size_t>(c_mine) * kPiece + kPiece - 1] : 0;
+    const uint32_t last_mine = start ? s.last[v_mine] : 0;
+    for (uint64_t todo = __ballot(start); todo; todo &= todo - 1) {
+        const uint32_t at_lane = static_cast<uint32_t>(__ffsll(static_cast<unsigned long long>(todo))) - 1, c = c0 + at_lane;
+        const uint32_t v = __builtin_amdgcn_readlane(v_mine, at_lane), last = __builtin_amdgcn_readlane(last_mine, at_lane);
+        const uint32_t n = (last - 1) / kPiece - c + 1, each = (n + kWaves - 1) / kWaves;
+        const uint32_t from = min(wave * each, n), to = min(from + each, n);
+        const float* slot = slots + 2 * static_cast<int64_t>(c) * dim;
+        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        uint32_t i = from;
+        if (i == 0) {
+            load_slab(slot + dim, col, dim, acc);
+            i = 1;
+        }
+        for (; i + 8 <= to; i += 8) {
+            float x[8][8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) load_slab(slot + 2 * static_cast<int64_t>(i + u) * dim, col, dim, x[u]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += x[u][j];
+        }
+        for (; i < to; ++i) {
+            float x[8];
+            load_slab(slot + 2 * static_cast<int64_t>(i) * dim, col, dim, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[j] += x[j];
+        }
+        if (wave > 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[wave - 1][lane + j * 64] = acc[j];
+        __syncthreads();
+        if (wave == 0) {
+            for (uint32_t u = 1; u < kWaves; ++u)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += sums[u - 1][lane + j * 64];
+            put_row(out + static_cast<int64_t>(v) * dim, col, dim, scale, accumulate, acc);
+        }
+        __syncthreads();
     }
 }
 
 // ---------------------------------------------------------------- host side
 
 struct Layout {
-    size_t key[2], entry[2], bounds, counts, slots, bytes;
+    size_t key[2], entry[2], last, starts, counts, totals, slots, bytes;
 };
 
 int64_t sort_blocks(int64_t E) { return ceil_div(E, kSortTile); }
@@ -394,9 +470,12 @@ Layout layout_of(int64_t E, int64_t rows, int64_t dim) {
     l.entry[0] = take(4 * E);
     l.key[1] = radix ? take(4 * E) : 0;
     l.entry[1] = radix ? take(4 * E) : 0;
-    l.bounds = take(8 * rows);
+    l.last = take(4 * rows);
     l.counts = radix ? take(4 * kBins * sort_blocks(E)) : 0;
-    l.slots = E > kPiece ? take(static_cast<size_t>(2 * ceil_div(E, kPiece)) * dim * 4) : 0;
+    l.totals = radix ? take(4 * kBins) : 0;
+    const int64_t pieces = ceil_div(E, radix ? kManyPiece : kFewPiece);
+    l.starts = take(4 * pieces);
+    l.slots = pieces > 1 ? take(static_cast<size_t>(2 * pieces) * dim * 4) : 0;
     l.bytes = at;
     return l;
 }
@@ -405,60 +484,70 @@ template <typename I>
 lsgd_status sort_tokens(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_t rows, const Layout& l, char* ws,
                         Sorted& s, hipStream_t st) {
     auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
-    s.first = u32(l.bounds);
-    s.last = s.first + rows;
-    const int64_t n = 2ll * rows;
-    hipLaunchKernelGGL(clear_bounds_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(2048, ceil_div(n, kBlock)))),
-                       dim3(kBlock), 0, st, s.first, n);
-    LSGD_TRY(check_launch("lsgd_embed_grad"));
+    s.last = u32(l.last);
+    s.starts = u32(l.starts);
+    const unsigned clears = static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(rows, 4 * kBlock)));
     if (E <= kRankMax) {
         s.key = u32(l.key[0]);
         s.entry = u32(l.entry[0]);
+        hipLaunchKernelGGL(clear_kernel, dim3(clears), dim3(kBlock), 0, st, s.last, rows);
         hipLaunchKernelGGL((rank_kernel<I>), dim3((E + 63) / 64), dim3(1024), 0, st, w, n_tokens, E, rows, s);
         return check_launch("lsgd_embed_grad");
     }
     const unsigned blocks = static_cast<unsigned>(sort_blocks(E));
-    uint32_t* counts = u32(l.counts);
+    uint32_t *counts = u32(l.counts), *totals = blocks > kOwnSums ? u32(l.totals) : nullptr;
     int from = 0;
     for (int shift = 0; shift == 0 || rows >> shift; shift += kDigitBits) {   // keys reach `rows`
         const uint32_t *key = u32(l.key[from]), *entry = u32(l.entry[from]);
         uint32_t *key_out = u32(l.key[1 - from]), *entry_out = u32(l.entry[1 - from]);
         if (shift == 0)
-            hipLaunchKernelGGL((digit_count_kernel<I, true>), dim3(blocks), dim3(kBlock), 0, st, w, key, n_tokens, E,
-                               rows, shift, counts);
+            hipLaunchKernelGGL((digit_count_kernel<I, true>), dim3(blocks + clears), dim3(kSortThreads), 0, st, w, key,
+                               n_tokens, E, rows, shift, blocks, counts, s.last);
         else
-            hipLaunchKernelGGL((digit_count_kernel<I, false>), dim3(blocks), dim3(kBlock), 0, st, w, key, n_tokens, E,
-                               rows, shift, counts);
-        hipLaunchKernelGGL(running_sum_kernel, dim3(1), dim3(1024), 0, st, counts, kBins * blocks);
+            hipLaunchKernelGGL((digit_count_kernel<I, false>), dim3(blocks), dim3(kSortThreads), 0, st, w, key, n_tokens,
+                               E, rows, shift, blocks, counts, s.last);
+        if (totals)
+            hipLaunchKernelGGL(block_sums_kernel, dim3(kBins / 64), dim3(512), 0, st, counts, blocks, totals);
         if (shift == 0)
-            hipLaunchKernelGGL((digit_place_kernel<I, true>), dim3(blocks), dim3(kBlock), 0, st, w, key, entry,
-                               n_tokens, E, rows, shift, counts, key_out, entry_out);
+            hipLaunchKernelGGL((digit_place_kernel<I, true>), dim3(blocks), dim3(kSortThreads), 0, st, w, key, entry,
+                               n_tokens, E, rows, shift, counts, totals, key_out, entry_out);
         else
-            hipLaunchKernelGGL((digit_place_kernel<I, false>), dim3(blocks), dim3(kBlock), 0, st, w, key, entry,
-                               n_tokens, E, rows, shift, counts, key_out, entry_out);
+            hipLaunchKernelGGL((digit_place_kernel<I, false>), dim3(blocks), dim3(kSortThreads), 0, st, w, key, entry,
+                               n_tokens, E, rows, shift, counts, totals, key_out, entry_out);
         LSGD_TRY(check_launch("lsgd_embed_grad"));
         from = 1 - from;
     }
     s.key = u32(l.key[from]);
     s.entry = u32(l.entry[from]);
-    hipLaunchKernelGGL(row_bounds_kernel, dim3((E + kBlock - 1) / kBlock), dim3(kBlock), 0, st, s, E, rows);
+    hipLaunchKernelGGL(row_ends_kernel, dim3((E + kBlock - 1) / kBlock), dim3(kBlock), 0, st, s, E, rows);
     return check_launch("lsgd_embed_grad");
+}
+
+template <int kPiece, typename GT, typename OT>
+lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim,
+                     float scale, float* slots, void* out, bool accumulate, hipStream_t st) {
+    const int64_t slabs = ceil_div(dim, 512), pieces = ceil_div(E, kPiece);
+    const int64_t piece_blocks = ceil_div(pieces * slabs, kBlock / 64);
+    const int64_t zero_blocks = accumulate ? 0 : std::min<int64_t>(1 << 20, ceil_div(rows, kZeroRows));
+    hipLaunchKernelGGL((sum_pieces_kernel<kPiece, GT, OT>), dim3(static_cast<unsigned>(piece_blocks + zero_blocks)),
+                       dim3(kBlock), 0, st, w, s, n_tokens, E, rows, dim, static_cast<uint32_t>(slabs), scale,
+                       static_cast<uint32_t>(piece_blocks), slots, static_cast<OT*>(out), accumulate);
+    LSGD_TRY(check_launch("lsgd_embed_grad"));
+    if (pieces > 1) {
+        hipLaunchKernelGGL((join_pieces_kernel<kPiece, OT>), dim3(static_cast<unsigned>(ceil_div(pieces, kJoin) * slabs)),
+                           dim3(kJoinThreads), 0, st, s, static_cast<uint32_t>(pieces), dim, static_cast<uint32_t>(slabs), scale,
+                           slots, static_cast<OT*>(out), accumulate);
+        LSGD_TRY(check_launch("lsgd_embed_grad"));
+    }
+    return LSGD_OK;
 }
 
 template <typename GT, typename OT>
 lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim,
                      float scale, float* slots, void* out, bool accumulate, hipStream_t st) {
-    const uint32_t slabs = static_cast<uint32_t>(ceil_div(dim, 512));
-    if (E > kPiece) {
-        const int64_t items = ceil_div(E, kPiece) * slabs;
-        hipLaunchKernelGGL((piece_sums_kernel<GT>), dim3(static_cast<unsigned>(ceil_div(items, kBlock / 64))),
-                           dim3(kBlock), 0, st, w, s, n_tokens, E, rows, dim, slabs, slots);
-        LSGD_TRY(check_launch("lsgd_embed_grad"));
-    }
-    hipLaunchKernelGGL((row_sums_kernel<GT, OT>), dim3(static_cast<unsigned>(std::min<int64_t>(kMaxGridBlocks, ceil_div(rows, kRowsPerBlock)))),
-                       dim3(kBlock), 0, st, w, s, n_tokens, rows, dim, slabs, scale, slots, static_cast<OT*>(out),
-                       accumulate);
-    return check_launch("lsgd_embed_grad");
+    return E > kRankMax
+               ? sum_rows<kManyPiece, GT, OT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st)
+               : sum_rows<kFewPiece, GT, OT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st);
 }
 
 lsgd_status check_index_type(lsgd_index_type it) {
@@ -470,7 +559,8 @@ lsgd_status check_grad_sizes(int32_t n_workers, int64_t n_tokens, int64_t rows, 
     if (n_workers < 1 || n_workers > LSGD_MAX_WORKERS)
         return fail(LSGD_ERR_SIZE, "n_workers=%d outside [1, %d]", n_workers, LSGD_MAX_WORKERS);
     LSGD_TRY(check_size(n_tokens, "n_tokens"));
-    LSGD_TRY(check_size(n_tokens * n_workers, "n_workers * n_tokens"));
+    if (n_tokens * n_workers > kMaxEntries)
+        return fail(LSGD_ERR_SIZE, "n_workers * n_tokens=%lld above 2^28", static_cast<long long>(n_tokens * n_workers));
     LSGD_TRY(check_size(rows, "rows"));
     LSGD_TRY(check_size(dim, "dim"));
     LSGD_TRY(check_matrix(n_tokens * n_workers, dim, "gradients"));

@@ -83,6 +83,7 @@ inline int64_t scales_bytes(int64_t rows, int64_t cols, int64_t block) {
 // element, and gfx950 loads and stores them with one 128-bit instruction.
 typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_u2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_u2 __attribute__((ext_vector_type(2), aligned(2)));
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t h) { return __builtin_bit_cast(float, h << 16); }
 
@@ -137,6 +138,87 @@ __device__ __forceinline__ void store8(uint16_t* p, int k, const float (&x)[8]) 
         for (int i = 0; i < 8; ++i)
             if (i < k) p[i] = static_cast<uint16_t>(f32_to_bf16(x[i]));
     }
+}
+
+// A wave's 512 columns from `col` on, in two halves of 256 with 4 neighbours per
+// lane each (col: the lane's first), so that every instruction of a wave covers
+// whole cache lines; elements past `dim` read as 0 and are not written. (8
+// neighbours per lane leave two binary32 stores of 16 bytes with gaps of 16, which
+// wrote at 4.3 TB/s instead of 6.)
+__device__ __forceinline__ int64_t slab_column(int64_t slab, uint32_t lane) { return slab * 512 + lane * 4; }
+
+__device__ __forceinline__ void load4(const float* p, int k, float* x) {
+    if (k >= 4) {
+        const f32x4_u a = *reinterpret_cast<const f32x4_u*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = a[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < k ? p[i] : 0.0f;
+    }
+}
+__device__ __forceinline__ void load4(const uint16_t* p, int k, float* x) {
+    if (k >= 4) {
+        const u32x2_u2 a = *reinterpret_cast<const u32x2_u2*>(p);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            x[2 * i] = bf16_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i < k ? bf16_to_f32(p[i]) : 0.0f;
+    }
+}
+// The first k of four neighbours.
+__device__ __forceinline__ void store4(float* p, int k, f32x4 v) {
+    if (k >= 4) {
+        *reinterpret_cast<f32x4_u*>(p) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < k) p[i] = v[i];
+    }
+}
+__device__ __forceinline__ void store4(uint16_t* p, int k, f32x4 v) {
+    if (k >= 4) {
+        *reinterpret_cast<u32x2_u2*>(p) = u32x2_u2{f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < k) p[i] = static_cast<uint16_t>(f32_to_bf16(v[i]));
+    }
+}
+// row: the row's first element.
+template <typename T>
+__device__ __forceinline__ void load_slab(const T* row, int64_t col, int64_t dim, float (&x)[8]) {
+    const int64_t left = dim - col;
+    load4(row + col, static_cast<int>(min(left, static_cast<int64_t>(4))), x);
+    load4(row + col + 256, static_cast<int>(min(left - 256, static_cast<int64_t>(4))), x + 4);
+}
+// The same for a row that is read once only: it does not stay in the caches.
+__device__ __forceinline__ void load4_once(const float* p, int k, float* x) {
+    if (k < 4) return load4(p, k, x);
+    const f32x4_u a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i];
+}
+__device__ __forceinline__ void load4_once(const uint16_t* p, int k, float* x) {
+    if (k < 4) return load4(p, k, x);
+    const u32x2_u2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x2_u2*>(p));
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        x[2 * i] = bf16_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+}
+template <typename T>
+__device__ __forceinline__ void load_slab_once(const T* row, int64_t col, int64_t dim, float (&x)[8]) {
+    const int64_t left = dim - col;
+    load4_once(row + col, static_cast<int>(min(left, static_cast<int64_t>(4))), x);
+    load4_once(row + col + 256, static_cast<int>(min(left - 256, static_cast<int64_t>(4))), x + 4);
+}
+template <typename T>
+__device__ __forceinline__ void store_slab(T* row, int64_t col, int64_t dim, const float (&x)[8]) {
+    const int64_t left = dim - col;
+    store4(row + col, static_cast<int>(min(left, static_cast<int64_t>(4))), f32x4{x[0], x[1], x[2], x[3]});
+    store4(row + col + 256, static_cast<int>(min(left - 256, static_cast<int64_t>(4))), f32x4{x[4], x[5], x[6], x[7]});
 }
 
 // |x| where x is finite, else 0.

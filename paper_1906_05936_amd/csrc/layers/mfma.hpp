@@ -11,7 +11,6 @@ namespace layers {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x2_u2 __attribute__((ext_vector_type(2), aligned(2)));
 
 template <typename F, int... I>
 __device__ __forceinline__ void unrolled_impl(const F& f, std::integer_sequence<int, I...>) {
@@ -149,26 +148,6 @@ struct Product<true> {
 
 __device__ __forceinline__ float value_of(float x) { return x; }
 __device__ __forceinline__ float value_of(uint16_t x) { return bf16_to_f32(x); }
-
-// The first k (1 to 4) of four neighbouring outputs.
-__device__ __forceinline__ void store4(float* p, int k, f32x4 v) {
-    if (k == 4) {
-        *reinterpret_cast<f32x4_u*>(p) = v;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < k) p[i] = v[i];
-    }
-}
-__device__ __forceinline__ void store4(uint16_t* p, int k, f32x4 v) {
-    if (k == 4) {
-        *reinterpret_cast<u32x2_u2*>(p) = u32x2_u2{f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3])};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < k) p[i] = static_cast<uint16_t>(f32_to_bf16(v[i]));
-    }
-}
 
 }  // namespace layers
 }  // namespace lsgd
