@@ -2,7 +2,8 @@
 buffers in a language model. Argument marshalling only, as in _lib.
 
 ``embed_lookup``, ``embed_grad``, ``quant8``, ``copy_out8``, ``matmul8`` and
-``weight_grad8`` mirror the C entry points; ``empty8`` allocates an 8-bit
+``weight_grad8`` mirror the C entry points (each tries the extension _marshal
+first, as _lib's calls do); ``empty8`` allocates an 8-bit
 matrix: codes (float8_e4m3fn, rows by pitch8(cols)) and scales (float8_e8m0fnu,
 ceil(rows/block) by scale_pitch8(cols)). uint8 tensors of the same bytes do too.
 """
@@ -11,7 +12,8 @@ import math
 
 import torch
 
-from ._lib import (_common_dtype, _dev_tensor, _dtype_code, _on, _stream, check, lib, ptr_array)
+from . import _lib
+from ._lib import (_common_dtype, _dev_tensor, _dtype_code, _native_target, _on, _stream, check, lib, ptr_array)
 
 EXPORTS = ("lsgd_embed_lookup", "lsgd_embed_grad_workspace_size", "lsgd_embed_grad", "lsgd_pitch8",
            "lsgd_scale_pitch8", "lsgd_quant8", "lsgd_copy_out8", "lsgd_matmul8",
@@ -99,6 +101,11 @@ def embed_lookup(table, tokens, out, scale=1.0, stream=None):
     """lsgd_embed_lookup: out[i] = scale * table[tokens[i]], 0 for a token
     outside the table. table: rows by dim (float32 or bfloat16); tokens: int32
     or int64, any shape; out: tokens.numel() by dim elements (float32 or bfloat16)."""
+    target = _native_target(table, stream)
+    if target is not None:
+        st = _lib._marshal.embed_lookup(table, tokens, out, scale, *target)
+        if st is not None:
+            return check(st)
     rows, dim = _matrix(table, "table")
     dev = table.device
     _dev_tensor(tokens, "tokens", None, None, dev)
@@ -126,6 +133,11 @@ def embed_grad(grads, tokens, out, scale=1.0, accumulate=False, workspace=None, 
     (float32 or bfloat16). workspace: a uint8 device tensor of
     embed_grad_workspace_size() bytes, 256-byte aligned; by default one is
     allocated for the call."""
+    target = _native_target(out, stream)
+    if target is not None and workspace is None and stream is None:
+        st = _lib._marshal.embed_grad(grads, tokens, out, scale, 1 if accumulate else 0, *target)
+        if st is not None:
+            return check(st)
     rows, dim = _matrix(out, "out")
     dev = out.device
     if not grads or len(tokens) != len(grads):
@@ -150,6 +162,11 @@ def embed_grad(grads, tokens, out, scale=1.0, accumulate=False, workspace=None, 
 def quant8(x, codes, scales, stream=None):
     """lsgd_quant8: x (float32 or bfloat16, rows by cols of its last dimension)
     in 8 bits, a scale per row and 128 columns. codes, scales: as empty8(rows, cols)."""
+    target = _native_target(x, stream)
+    if target is not None:
+        st = _lib._marshal.quant8(x, codes, scales, *target)
+        if st is not None:
+            return check(st)
     rows, cols = _matrix(x, "x")
     dev = x.device
     q = _bytes8(codes, "codes", _CODES, rows * pitch8(cols), dev)
@@ -165,6 +182,11 @@ def copy_out8(params, replicas=(), transposed=(), stream=None):
     a scale per 128 rows and 128 columns; every one of `transposed` = its
     transpose. replicas, transposed: lists of (codes, scales) as empty8(rows,
     cols, 128) and empty8(cols, rows, 128)."""
+    target = _native_target(params, stream)
+    if target is not None:
+        st = _lib._marshal.copy_out8(params, replicas, transposed, *target)
+        if st is not None:
+            return check(st)
     rows, cols = _matrix(params, "params", torch.float32)
     dev = params.device
     arrays = []
@@ -203,6 +225,11 @@ def matmul8(a, a_scales, b, b_scales, out, stream=None):
     matrices a (m rows) and b (n rows) of the same pitch (block 1 or 128, by
     their scales' number); out: m by n, float32 (exact products) or bfloat16
     (the faster matrix instructions)."""
+    target = _native_target(a, stream)
+    if target is not None:
+        st = _lib._marshal.matmul8(a, a_scales, b, b_scales, out, *target)
+        if st is not None:
+            return check(st)
     pa, sa, ba, m, pitch = _operand8(a, a_scales, "a")
     dev = a.device
     pb, sb, bb, n, pitch_b = _operand8(b, b_scales, "b", dev)
@@ -227,6 +254,11 @@ def weight_grad8(grad, x, x_scales, out, accumulate=False, workspace=None, strea
     out[j][c] with accumulate). grad: m by n, bfloat16; x: m by k in 8 bits, a
     scale per row and 128 columns (as quant8 writes it); out: n by k, float32
     or bfloat16. workspace: as embed_grad's, of weight_grad8_workspace_size() bytes."""
+    target = _native_target(out, stream)
+    if target is not None and workspace is None and stream is None:
+        st = _lib._marshal.weight_grad8(grad, x, x_scales, out, 1 if accumulate else 0, *target)
+        if st is not None:
+            return check(st)
     n, k = _matrix(out, "out")
     dev = out.device
     m, gn = _matrix(grad, "grad", torch.bfloat16, dev)

@@ -114,12 +114,15 @@ def zipf(n, rows, seed, dtype=torch.int64):
     (1000, 64, 4096, 1, torch.int64, "zipf"), (1000, 64, 4097, 1, torch.int64, "zipf"),
     (511, 24, 1400, 3, torch.int32, "zipf"), (512, 24, 2100, 2, torch.int64, "any"), (3, 520, 5000, 1, torch.int64, "same"),
     (300000, 9, 2500, 2, torch.int64, "zipf"), (70, 16, 9000, 1, torch.int32, "outside"), (2000, 1032, 3000, 4, torch.int64, "zipf"),
-    (5, 8, 40000, 1, torch.int32, "any"), (40, 40, 50, 128, torch.int64, "zipf")])
+    (5, 8, 40000, 1, torch.int32, "any"), (40, 40, 50, 128, torch.int64, "zipf"), (90, 8, 300, 1, torch.int64, "padded"),
+    (300, 24, 6000, 2, torch.int32, "padded"), (6000, 520, 30000, 4, torch.int64, "zipf")])
 def test_grad(gdt, odt, rows, dim, n, workers, it, how):
     if how == "zipf":
         tokens = [zipf(n, rows, 10 + w, it) for w in range(workers)]
     elif how == "same":
         tokens = [torch.full((n,), rows - 1, device=DEV, dtype=it) for _ in range(workers)]
+    elif how == "padded":
+        tokens = [torch.where(torch.arange(n, device=DEV) % 3 == 0, zipf(n, rows, 10 + w, it), -1).to(it) for w in range(workers)]
     elif how == "outside":
         tokens = [torch.where(torch.arange(n, device=DEV) % 2 == 0, -5, rows).to(it) for _ in range(workers)]
     else:
@@ -576,3 +579,96 @@ def test_on_a_stream_of_its_own():
     lsgd.embed_lookup(table, tokens, x, stream=side)
     side.synchronize()
     assert torch.equal(out, want) and torch.equal(x, table[tokens])
+
+
+# ---------------------------------------------------------------- the binding's two paths
+
+def every_call():
+    """One call of each, as (name, function of nothing that returns its outputs)."""
+    table, tokens, x = randn(30, 72, seed=1), zipf(500, 30, 2), randn(500, 72, seed=3)
+    dy, p = randn(500, 40, seed=4, dtype=BF16), randn(40, 72, seed=5)
+
+    def lookup():
+        out = nans(500, 72, dtype=BF16)
+        lsgd.embed_lookup(table, tokens, out, 2)
+        return [out]
+
+    def grad():
+        out = nans(30, 72)
+        lsgd.embed_grad((x,), [tokens], out, scale=0.5)
+        return [out]
+
+    def quant():
+        return list(as8(x, 1))
+
+    def copy():
+        a, b, t = lsgd.empty8(40, 72, 128), lsgd.empty8(40, 72, 128), lsgd.empty8(72, 40, 128)
+        lsgd.copy_out8(p, [a, b], (t,))
+        return [*a, *b, *t]
+
+    def product():
+        out = nans(500, 40)
+        lsgd.matmul8(*as8(x, 1), *as8(p, 128), out)
+        return [out]
+
+    def weights():
+        out = randn(40, 72, seed=6)
+        lsgd.weight_grad8(dy, *as8(x, 1), out, accumulate=True)
+        return [out]
+    return {f.__name__: f for f in (lookup, grad, quant, copy, product, weights)}
+
+
+@pytest.mark.parametrize("name", ["lookup", "grad", "quant", "copy", "product", "weights"])
+def test_binding_paths_agree(name, monkeypatch):
+    from paper_1906_05936_amd import _lib
+    assert _lib._marshal is not None
+    native = every_call()[name]()
+    monkeypatch.setattr(_lib, "_marshal", None)
+    for a, b in zip(native, every_call()[name]()):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def refused():
+    x, t = randn(8, 16, seed=1), torch.zeros(8, dtype=torch.int64, device=DEV)
+    (q, s), (w, ws) = lsgd.empty8(8, 16), lsgd.empty8(4, 16, 128)
+    g = x[:, :4].bfloat16().contiguous()
+    return [
+        (TypeError, lambda: lsgd.embed_lookup(x.half(), t, x)),
+        (TypeError, lambda: lsgd.embed_lookup(x, t.short(), x)),
+        (ValueError, lambda: lsgd.embed_lookup(x, t, x[:7])),
+        (ValueError, lambda: lsgd.embed_lookup(x.t(), t, x)),
+        (ValueError, lambda: lsgd.embed_lookup(x, t.cpu(), x)),
+        (lsgd.LsgdError, lambda: lsgd.embed_lookup(x, t, x)),
+        (ValueError, lambda: lsgd.embed_grad([x], [t, t], x)),
+        (ValueError, lambda: lsgd.embed_grad([x, x], [t, t[:7]], x.clone())),
+        (TypeError, lambda: lsgd.embed_grad([x, x], [t, t.int()], x.clone())),
+        (TypeError, lambda: lsgd.embed_grad([x, x.bfloat16()], [t, t], x.clone())),
+        (lsgd.LsgdError, lambda: lsgd.embed_grad([x], [t], x)),
+        (lsgd.LsgdError, lambda: lsgd.embed_grad([x], [t], x.clone(), workspace=torch.empty(1, dtype=torch.uint8, device=DEV))),
+        (ValueError, lambda: lsgd.quant8(x, q[:7], s)),
+        (TypeError, lambda: lsgd.quant8(x, q.view(torch.int8), s)),
+        (TypeError, lambda: lsgd.quant8(x.double(), q, s)),
+        (ValueError, lambda: lsgd.copy_out8(x, [(q, s)])),
+        (TypeError, lambda: lsgd.copy_out8(x.bfloat16(), [])),
+        (ValueError, lambda: lsgd.matmul8(q, s, w, ws, x)),
+        (ValueError, lambda: lsgd.matmul8(q, s[:5], w, ws, x)),
+        (ValueError, lambda: lsgd.matmul8(q, s, *lsgd.empty8(4, 300), nans(8, 4))),
+        (TypeError, lambda: lsgd.matmul8(x, s, w, ws, nans(8, 4))),
+        (TypeError, lambda: lsgd.weight_grad8(x, q, s, nans(16, 16))),
+        (ValueError, lambda: lsgd.weight_grad8(g, q, s, nans(5, 16))),
+        (ValueError, lambda: lsgd.weight_grad8(g, q, s, nans(4, 200))),
+    ]
+
+
+@pytest.mark.parametrize("k", range(24))
+def test_refusals_agree(k, monkeypatch):
+    from paper_1906_05936_amd import _lib
+    kind, call = refused()[k]
+    texts = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(_lib, "_marshal", None)
+        with pytest.raises(kind) as e:
+            call()
+        texts.append(str(e.value))
+    assert texts[0] == texts[1]
