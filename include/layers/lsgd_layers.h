@@ -143,7 +143,8 @@ LSGD_API lsgd_status lsgd_matmul8(const void* a, const void* a_scales, int32_t a
  * The gradient of a linear layer's parameters from its activations in 8 bits:
  *   out[j][c] = sum over i < m of grad[i][j] * x[i][c]  (+ out[j][c] if accumulate)
  * grad: m x n, bfloat16 (the gradient of the layer's output); x: m x k in 8
- * bits, block 1; out: n x k of dtype odt, a worker's gradient buffer. Products
+ * bits, block 1; out: n x k of dtype odt, a worker's gradient buffer; n and k at
+ * most 2^24. Products
  * are exact (elements of x between 2^-126 and 2^128), sums binary32, rounded
  * once to odt. m == 0 gives 0 (with accumulate: a no-op); no-op where n or k is 0.
  * workspace as for lsgd_embed_grad; lsgd_weight_grad8_workspace_size may give 0

@@ -51,11 +51,18 @@ __device__ __forceinline__ void load_lds16(const void* global, void* lds) {
                                      0, 0);
 }
 
-// `bytes` from p on, addressed by a lane's 32-bit offset plus a uniform one.
+// `bytes` from p on, addressed by a lane's 32-bit offset (plus a uniform one, which
+// the hardware's bounds check leaves out). Loads past the end give 0.
 struct Buffer {
     __amdgpu_buffer_rsrc_t rsrc;
     __device__ __forceinline__ Buffer(const void* p, uint32_t bytes)
         : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000)) {}
+    __device__ __forceinline__ u32x4 load16(uint32_t offset) const {
+        return __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0);
+    }
+    __device__ __forceinline__ uint32_t load1(uint32_t offset) const {
+        return __builtin_amdgcn_raw_buffer_load_b8(rsrc, offset, 0, 0);
+    }
     // as load_lds16
     __device__ __forceinline__ void load_lds16(uint32_t offset, uint32_t uniform, void* lds) const {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, offset, uniform, 0, 0);
@@ -73,11 +80,33 @@ __device__ __forceinline__ void interleave_reads() {
     });
 }
 
+// The same for 16 matrix instructions: conversions and LDS writes between the first
+// half, so that the reads between the second do not wait behind them.
+__device__ __forceinline__ void interleave_writes() {
+    unrolled<8>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
+    });
+    unrolled<8>([](auto) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    });
+}
+
 // The workgroup's loads into LDS issued so far have arrived, and all its waves
-// are past their earlier LDS reads.
+// are past their earlier LDS accesses.
 __device__ __forceinline__ void loads_done() {
     __builtin_amdgcn_sched_barrier(0);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// The same where no loads into LDS are under way: loads into registers go on.
+__device__ __forceinline__ void lds_done() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);

@@ -148,7 +148,7 @@ def wgrad(g=A, x=B, s=C, m=1000, n=20, k=300, out=D, odt=0, acc=0, ws=E, size=64
 
 @pytest.mark.parametrize("bad,status", [
     (dict(odt=2), DTYPE), (dict(m=-1), SIZE), (dict(n=BIG), SIZE), (dict(k=-1), SIZE), (dict(m=BIG - 1, n=BIG - 1), SIZE),
-    (dict(n=65535 * 128 + 1, k=1), SIZE), (dict(g=None), NULL), (dict(x=None), NULL), (dict(s=None), NULL),
+    (dict(n=(1 << 24) + 1), SIZE), (dict(k=(1 << 24) + 1), SIZE), (dict(g=None), NULL), (dict(x=None), NULL), (dict(s=None), NULL),
     (dict(out=None), NULL), (dict(g=A + 8), ALIGN), (dict(x=B + 8), ALIGN), (dict(s=C + 4), ALIGN), (dict(out=D + 8), ALIGN),
     (dict(out=A), ALIAS), (dict(out=B), ALIAS), (dict(out=C), ALIAS), (dict(n=0, g=None, out=None), OK),
     (dict(k=0, x=None, out=None), OK), (dict(m=0, acc=1, g=None, out=None), OK)])
