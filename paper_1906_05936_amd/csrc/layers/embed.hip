@@ -14,27 +14,45 @@ __device__ __forceinline__ int64_t token_row(const I* tokens, int64_t i, int64_t
     return t >= 0 && t < rows ? t : -1;
 }
 
+// 16 bytes of a row of out from the same elements of a row of the table.
+template <typename TT>
+__device__ __forceinline__ void scaled_copy(const TT* t, float scale, float* o, int k) {
+    float x[4] = {0, 0, 0, 0};
+    if (t) load4(t, k, x);
+    const f32x4 v = f32x4{x[0], x[1], x[2], x[3]} * scale;
+    if (k < 4) return store4(o, k, v);
+    __builtin_nontemporal_store(f32x4_u{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_u*>(o));
+}
+template <typename TT>
+__device__ __forceinline__ void scaled_copy(const TT* t, float scale, uint16_t* o, int k) {
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (t) load8(t, k, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] *= scale;
+    if (k < 8) return store8(o, k, x);
+    u32x4_u2 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = f32_to_bf16x2(x[2 * i], x[2 * i + 1]);
+    __builtin_nontemporal_store(a, reinterpret_cast<u32x4_u2*>(o));
+}
+
 // A copy of rows: bound by the bytes of the rows read and written. A lane moves
-// 8 elements; `lanes` (a power of two) of them walk one row, so that a
-// workgroup holds 256 / lanes short rows or a part of a long one.
+// 16 bytes of out; `lanes` (a power of two) of them walk one row, so that a
+// workgroup holds 256 / lanes short rows or a part of a long one. 16384 rows of
+// 4096 bfloat16: 33 us, 8.2 TB/s counting every row read (frequent rows come from
+// the caches); with stores through the caches 43.
 template <typename TT, typename OT, typename I>
 __global__ __launch_bounds__(kBlock) void embed_lookup_kernel(const TT* __restrict__ table, int64_t rows, int64_t dim,
                                                               const I* __restrict__ tokens, int64_t n_tokens,
                                                               float scale, OT* __restrict__ out, int lanes) {
+    constexpr int kVec = 16 / sizeof(OT);
     const int per = kBlock / lanes;
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * per + threadIdx.x / lanes; i < n_tokens;
          i += static_cast<int64_t>(gridDim.x) * per) {
         const int64_t t = token_row(tokens, i, rows);
-        for (int64_t c = threadIdx.x % lanes * 8; c < dim; c += lanes * 8) {
-            const int k = static_cast<int>(dim - c < 8 ? dim - c : 8);
-            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (t >= 0) {
-                load8(table + t * dim + c, k, x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] *= scale;
-            }
-            store8(out + i * dim + c, k, x);
-        }
+        for (int64_t c = threadIdx.x % lanes * kVec; c < dim; c += lanes * kVec)
+            scaled_copy(t >= 0 ? table + t * dim + c : nullptr, scale, out + i * dim + c,
+                        static_cast<int>(min(dim - c, static_cast<int64_t>(kVec))));
     }
 }
 
@@ -42,7 +60,7 @@ template <typename TT, typename OT>
 void launch_lookup(const void* table, int64_t rows, int64_t dim, const void* tokens, lsgd_index_type it, int64_t n,
                    float scale, void* out, hipStream_t s) {
     int lanes = 1;
-    while (lanes < kBlock && lanes * 8 < dim) lanes *= 2;
+    while (lanes < kBlock && lanes * static_cast<int64_t>(16 / sizeof(OT)) < dim) lanes *= 2;
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(kMaxGridBlocks, ceil_div(n, kBlock / lanes))));
     if (it == LSGD_I32)
         hipLaunchKernelGGL((embed_lookup_kernel<TT, OT, int32_t>), grid, dim3(kBlock), 0, s,

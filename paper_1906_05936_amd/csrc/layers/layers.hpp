@@ -117,6 +117,21 @@ __device__ __forceinline__ void load8(const uint16_t* p, int k, float (&x)[8]) {
         for (int i = 0; i < 8; ++i) x[i] = i < k ? bf16_to_f32(p[i]) : 0.0f;
     }
 }
+// The same for what is read once only: it does not stay in the caches.
+__device__ __forceinline__ void load8_once(const float* p, int k, float (&x)[8]) {
+    if (k < 8) return load8(p, k, x);
+    const f32x4_u a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p));
+    const f32x4_u b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p + 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+__device__ __forceinline__ void load8_once(const uint16_t* p, int k, float (&x)[8]) {
+    if (k < 8) return load8(p, k, x);
+    const u32x4_u2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_u2*>(p));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[2 * i] = bf16_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
+}
 __device__ __forceinline__ void store8(float* p, int k, const float (&x)[8]) {
     if (k >= 8) {
         *reinterpret_cast<f32x4_u*>(p) = f32x4_u{x[0], x[1], x[2], x[3]};
@@ -194,7 +209,7 @@ __device__ __forceinline__ void load_slab(const T* row, int64_t col, int64_t dim
     load4(row + col, static_cast<int>(min(left, static_cast<int64_t>(4))), x);
     load4(row + col + 256, static_cast<int>(min(left - 256, static_cast<int64_t>(4))), x + 4);
 }
-// The same for a row that is read once only: it does not stay in the caches.
+// The same for a row that is read once only.
 __device__ __forceinline__ void load4_once(const float* p, int k, float* x) {
     if (k < 4) return load4(p, k, x);
     const f32x4_u a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p));

@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             for (int q = 0; q < 8; ++q) {
                 const uint32_t row = q * 4 + l / 16;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 256 + ((l % 16) ^ (row % 16)) * 16);
-                *reinterpret_cast<u32x4_u2*>(o + lane_at) = u32x4_u2{v[0], v[1], v[2], v[3]};
+                __builtin_nontemporal_store(u32x4_u2{v[0], v[1], v[2], v[3]}, reinterpret_cast<u32x4_u2*>(o + lane_at));
                 o += 4 * static_cast<uint64_t>(row_bytes);
             }
             __builtin_amdgcn_sched_barrier(0);
