@@ -90,11 +90,14 @@ constexpr int kSortTile = kSortThreads * kSortRounds;   // entries a workgroup o
 constexpr int kDigitBits = 9;              // two passes for tables of up to 2^18 - 1 rows
 constexpr int kBins = 1 << kDigitBits;
 constexpr int kOwnSums = 256;              // up to so many workgroups each add up the counts before its own
-constexpr int kRankMax = 4096;             // entries that are sorted by counting smaller ones
-// Sorted entries in a piece, which a wave's lanes hold: with few entries latency
-// counts, and 16 in a row are faster (509 entries: 24 us, with 32 30, with 64 46);
-// with many, the slots' bytes (131072 entries: 432, 413, 417 us).
-constexpr int kFewPiece = 8, kManyPiece = 32, kFewAhead = 8, kManyAhead = 4;
+constexpr int kRankBits = 13, kRankMax = 1 << kRankBits;   // entries that are sorted by counting smaller ones
+// Sorted entries in a piece, which a wave's lanes hold: where the pieces are few,
+// latency counts and a wave takes 8 (509 entries of 203 binary32: 22 us, with 16 24,
+// with 32 30), else 32, as the slots cost bytes (131072 of 2048 bfloat16: 413 us,
+// with 16 432).
+constexpr int kFewPiece = 8, kManyPiece = 32;
+constexpr int64_t kFewWaves = 1 << 14;
+int piece_of(int64_t E, int64_t dim) { return E * ceil_div(dim, 512) <= kFewWaves * kFewPiece ? kFewPiece : kManyPiece; }
 constexpr int64_t kMaxEntries = 1 << 28;   // grids over pieces stay within a dispatch
 
 struct Workers {
@@ -105,7 +108,7 @@ struct Workers {
 struct Sorted {
     uint32_t* key;     // [E] row, or `rows` for tokens outside the table
     uint32_t* entry;   // [E]
-    uint32_t* last;    // [rows] end of the row's entries, 0 for a row without
+    uint32_t* last;    // many entries only: [rows] end of the row's entries, 0 for a row without
     uint32_t* starts;  // [pieces] whether a row of several pieces starts in it
 };
 
@@ -124,41 +127,66 @@ __device__ __forceinline__ void clear(uint32_t* p, uint32_t n, uint32_t block, u
         p[i] = 0;
 }
 
-__global__ __launch_bounds__(kBlock) void clear_kernel(uint32_t* __restrict__ p, uint32_t n) {
-    clear(p, n, blockIdx.x, gridDim.x);
+// Zeros into the rows v0 + r, r < n <= 64, whose bit in `rows` is set: a workgroup of
+// `waves` waves, 512 columns of a row at a time each.
+template <typename OT>
+__device__ __forceinline__ void zero_rows(OT* out, uint64_t v0, uint64_t rows, uint32_t n, int64_t dim, uint32_t slabs,
+                                          uint32_t wave, uint32_t waves, uint32_t lane) {
+    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (uint32_t item = wave; item < n * slabs; item += waves)
+        if (rows >> (item / slabs) & 1)
+            store_slab(out + static_cast<int64_t>(v0 + item / slabs) * dim, slab_column(item % slabs, lane), dim, zero);
 }
 
-// Rank of an entry = entries with a smaller key + earlier entries with the same
-// one. A workgroup ranks 64 entries, its 16 waves counting over a sixteenth of
-// all entries each; E^2 comparisons in one launch, against four for the radix
-// sort (which takes over where E^2 shows).
-template <typename I>
-__global__ __launch_bounds__(1024) void rank_kernel(Workers w, uint32_t n_tokens, uint32_t E, uint32_t rows, Sorted s) {
-    __shared__ uint32_t keys[kRankMax];
-    __shared__ uint32_t part[3][16][64];
-    for (uint32_t e = threadIdx.x; e < E; e += 1024) keys[e] = key_of<I>(w, e, n_tokens, rows);
-    __syncthreads();
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t e0 = blockIdx.x * 64, e = e0 + lane;
-    const uint32_t k = e < E ? keys[e] : 0;
-    const uint32_t span = (E + 15) / 16, j0 = min(wave * span, E), j1 = min(j0 + span, E);
-    uint32_t lt = 0, eq = 0, before = 0;
-    for (uint32_t j = j0; j < j1; ++j) {
-        const uint32_t q = keys[j];
-        lt += q < k;
-        eq += q == k;
-        before += q == k && j < e;
+// Few entries. Key and entry in one number of type K; the rank of an entry is how many
+// are smaller: each of the first ceil(E / 64) workgroups ranks 64, its 16 waves
+// counting over a sixteenth of all entries each; E^2 comparisons in one launch,
+// against five for the radix sort (which takes over where E^2 shows). The other
+// workgroups write zeros into the rows without entries, 64 rows each, which they
+// find among the tokens themselves.
+template <typename K, typename I, typename OT>
+__global__ __launch_bounds__(1024) void rank_kernel(Workers w, uint32_t n_tokens, uint32_t E, uint32_t rows, Sorted s,
+                                                    OT* __restrict__ out, int64_t dim, uint32_t slabs) {
+    __shared__ __align__(16) K keys[kRankMax];
+    __shared__ uint32_t part[16][64];
+    __shared__ uint32_t has[2];   // a bit for each of 64 rows
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t ranking = (E + 63) / 64;
+    if (blockIdx.x >= ranking) {
+        for (uint64_t v0 = static_cast<uint64_t>(blockIdx.x - ranking) * 64; v0 < rows;
+             v0 += static_cast<uint64_t>(gridDim.x - ranking) * 64) {
+            if (threadIdx.x < 2) has[threadIdx.x] = 0;
+            __syncthreads();
+            for (uint32_t e = threadIdx.x; e < E; e += 1024) {
+                const uint64_t r = key_of<I>(w, e, n_tokens, rows) - v0;
+                if (r < 64) atomicOr(&has[r / 32], 1u << (r % 32));
+            }
+            __syncthreads();
+            const uint64_t empty = ~(static_cast<uint64_t>(has[1]) << 32 | has[0]);
+            zero_rows(out, v0, empty, static_cast<uint32_t>(min(static_cast<uint64_t>(64), rows - v0)), dim, slabs, wave, 16,
+                      lane);
+            __syncthreads();
+        }
+        return;
     }
-    part[0][wave][lane] = lt;
-    part[1][wave][lane] = eq;
-    part[2][wave][lane] = before;
+    const uint32_t span = (E + 63) / 64 * 4;   // of a wave, filled up with numbers that are smaller than none
+    for (uint32_t e = threadIdx.x; e < 16 * span; e += 1024)
+        keys[e] = e < E ? static_cast<K>(key_of<I>(w, e, n_tokens, rows)) << kRankBits | e : ~K{0};
+    __syncthreads();
+    const uint32_t e = blockIdx.x * 64 + lane;
+    const K mine = keys[min(e, E - 1)];
+    uint32_t smaller = 0;
+#pragma unroll 4
+    for (uint32_t j = wave * span; j < (wave + 1) * span; j += 4)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) smaller += keys[j + u] < mine;
+    part[wave][lane] = smaller;
     __syncthreads();
     if (wave == 0 && e < E) {
-        lt = eq = before = 0;
-        for (int i = 0; i < 16; ++i) lt += part[0][i][lane], eq += part[1][i][lane], before += part[2][i][lane];
-        s.key[lt + before] = k;
-        s.entry[lt + before] = e;
-        if (k < rows && before == 0) s.last[k] = lt + eq;
+        uint32_t rank = 0;
+        for (int i = 0; i < 16; ++i) rank += part[i][lane];
+        s.key[rank] = static_cast<uint32_t>(mine >> kRankBits);
+        s.entry[rank] = e;
     }
 }
 
@@ -334,15 +362,11 @@ __global__ __launch_bounds__(kBlock) void sum_pieces_kernel(Workers w, Sorted s,
                                                             OT* __restrict__ out, bool accumulate) {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (blockIdx.x >= piece_blocks) {
-        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         const uint32_t stride = (gridDim.x - piece_blocks) * kZeroRows;
         for (uint64_t v0 = static_cast<uint64_t>(blockIdx.x - piece_blocks) * kZeroRows; v0 < rows; v0 += stride) {
             const uint32_t n = min(kZeroRows, static_cast<uint32_t>(rows - v0));
             const uint64_t empty = __ballot(lane < n && (E == 0 || s.last[v0 + min(lane, n - 1)] == 0));
-            for (uint32_t item = wave; item < n * slabs; item += kBlock / 64) {
-                if (empty >> (item / slabs) & 1)
-                    store_slab(out + static_cast<int64_t>(v0 + item / slabs) * dim, slab_column(item % slabs, lane), dim, zero);
-            }
+            zero_rows(out, v0, empty, n, dim, slabs, wave, kBlock / 64, lane);
         }
         return;
     }
@@ -381,7 +405,8 @@ __global__ __launch_bounds__(kBlock) void sum_pieces_kernel(Workers w, Sorted s,
         return reinterpret_cast<const GT*>(static_cast<uint64_t>(h) << 32 | l);
     };
     float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    constexpr int kAhead = kPiece == kFewPiece ? kFewAhead : kManyAhead;   // rows whose loads are in flight
+    // rows whose loads are under way (131072 entries of 2048: 4 360 us, 8 367, without once-only loads 373 and 413)
+    constexpr int kAhead = 4;
     bool slot_first = first;
     for (uint32_t j = from; j < to; j += kAhead) {
         float x[kAhead][8];
@@ -407,6 +432,21 @@ __global__ __launch_bounds__(kBlock) void sum_pieces_kernel(Workers w, Sorted s,
     }
 }
 
+// How many pieces behind piece c begin with row v, which fills the first of them.
+template <int kPiece>
+__device__ __forceinline__ uint32_t pieces_behind(const uint32_t* key, uint32_t c, uint32_t pieces, uint32_t v) {
+    const uint32_t lane = threadIdx.x & 63;
+    uint32_t step = 1, lo = c + 1, hi = pieces;   // piece lo begins with v; the 64 from it on, then all others
+    for (;;) {
+        const uint64_t at = lo + static_cast<uint64_t>(lane) * step;
+        const uint32_t n = __popcll(__ballot(at < hi && key[min(at, static_cast<uint64_t>(hi - 1)) * kPiece] == v));
+        lo += (n - 1) * step;
+        if (step == 1 && (n < 64 || lo + 1 >= hi)) return lo - c;
+        if (step > 1) hi = min(hi, lo + step);
+        step = max(1u, (hi - lo + 63) / 64);
+    }
+}
+
 // Rows of several pieces: a workgroup adds the slot 2c + 1 of the piece c in which
 // the row starts and the following pieces' slots 2c, divided over its waves in
 // order, then the waves' sums in order. It looks at kJoin pieces, 512 columns.
@@ -425,11 +465,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_pieces_kernel(Sorted s, uin
     const uint32_t c_mine = c0 + lane;
     const bool start = lane < kJoin && c_mine < pieces && s.starts[c_mine] != 0;
     const uint32_t v_mine = start ? s.key[static_cast<size_t>(c_mine) * kPiece + kPiece - 1] : 0;
-    const uint32_t last_mine = start ? s.last[v_mine] : 0;
+    const uint32_t last_mine = start && s.last ? s.last[v_mine] : 0;
     for (uint64_t todo = __ballot(start); todo; todo &= todo - 1) {
         const uint32_t at_lane = static_cast<uint32_t>(__ffsll(static_cast<unsigned long long>(todo))) - 1, c = c0 + at_lane;
         const uint32_t v = __builtin_amdgcn_readlane(v_mine, at_lane), last = __builtin_amdgcn_readlane(last_mine, at_lane);
-        const uint32_t n = (last - 1) / kPiece - c + 1, each = (n + kWaves - 1) / kWaves;
+        const uint32_t n = s.last ? (last - 1) / kPiece - c + 1 : 1 + pieces_behind<kPiece>(s.key, c, pieces, v), each = (n + kWaves - 1) / kWaves;
         const uint32_t from = min(wave * each, n), to = min(from + each, n);
         const float* slot = slots + 2 * static_cast<int64_t>(c) * dim;
         float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -488,30 +528,39 @@ Layout layout_of(int64_t E, int64_t rows, int64_t dim) {
     l.entry[0] = take(4 * E);
     l.key[1] = radix ? take(4 * E) : 0;
     l.entry[1] = radix ? take(4 * E) : 0;
-    l.last = take(4 * rows);
+    l.last = radix ? take(4 * rows) : 0;
     l.counts = radix ? take(4 * kBins * sort_blocks(E)) : 0;
     l.totals = radix ? take(4 * kBins) : 0;
-    const int64_t pieces = ceil_div(E, radix ? kManyPiece : kFewPiece);
+    const int64_t pieces = ceil_div(E, piece_of(E, dim));
     l.starts = take(4 * pieces);
     l.slots = pieces > 1 ? take(static_cast<size_t>(2 * pieces) * dim * 4) : 0;
     l.bytes = at;
     return l;
 }
 
-template <typename I>
-lsgd_status sort_tokens(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_t rows, const Layout& l, char* ws,
-                        Sorted& s, hipStream_t st) {
+// Sorts the entries; few of them: fills out's rows without entries as well, unless
+// `out` is null.
+template <typename I, typename OT>
+lsgd_status sort_tokens(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim, const Layout& l,
+                        char* ws, Sorted& s, OT* out, hipStream_t st) {
     auto u32 = [&](size_t off) { return reinterpret_cast<uint32_t*>(ws + off); };
-    s.last = u32(l.last);
     s.starts = u32(l.starts);
-    const unsigned clears = static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(rows, 4 * kBlock)));
     if (E <= kRankMax) {
         s.key = u32(l.key[0]);
         s.entry = u32(l.entry[0]);
-        hipLaunchKernelGGL(clear_kernel, dim3(clears), dim3(kBlock), 0, st, s.last, rows);
-        hipLaunchKernelGGL((rank_kernel<I>), dim3((E + 63) / 64), dim3(1024), 0, st, w, n_tokens, E, rows, s);
+        const int64_t zeros = out ? std::min<int64_t>(4096, ceil_div(rows, 64)) : 0;
+        const dim3 grid(static_cast<unsigned>((E + 63) / 64 + zeros));
+        const uint32_t slabs = static_cast<uint32_t>(ceil_div(dim, 512));
+        if (rows < 1u << (32 - kRankBits))   // keys reach `rows`
+            hipLaunchKernelGGL((rank_kernel<uint32_t, I, OT>), grid, dim3(1024), 0, st, w, n_tokens, E, rows, s, out, dim,
+                               slabs);
+        else
+            hipLaunchKernelGGL((rank_kernel<uint64_t, I, OT>), grid, dim3(1024), 0, st, w, n_tokens, E, rows, s, out, dim,
+                               slabs);
         return check_launch("lsgd_embed_grad");
     }
+    s.last = u32(l.last);
+    const unsigned clears = static_cast<unsigned>(std::min<int64_t>(1024, ceil_div(rows, 4 * kBlock)));
     const unsigned blocks = static_cast<unsigned>(sort_blocks(E));
     uint32_t *counts = u32(l.counts), *totals = blocks > kOwnSums ? u32(l.totals) : nullptr;
     int from = 0;
@@ -542,19 +591,20 @@ lsgd_status sort_tokens(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_
 }
 
 template <int kPiece, typename GT, typename OT>
-lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim,
-                     float scale, float* slots, void* out, bool accumulate, hipStream_t st) {
+lsgd_status sum_rows_of(const Workers& w, const Sorted& s, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim,
+                        float scale, float* slots, OT* out, bool accumulate, hipStream_t st) {
     const int64_t slabs = ceil_div(dim, 512), pieces = ceil_div(E, kPiece);
     const int64_t piece_blocks = ceil_div(pieces * slabs, kBlock / 64);
-    const int64_t zero_blocks = accumulate ? 0 : std::min<int64_t>(1 << 20, ceil_div(rows, kZeroRows));
+    const bool zeroed = E > 0 && E <= kRankMax;   // by the launch that sorted
+    const int64_t zero_blocks = accumulate || zeroed ? 0 : std::min<int64_t>(1 << 20, ceil_div(rows, kZeroRows));
     hipLaunchKernelGGL((sum_pieces_kernel<kPiece, GT, OT>), dim3(static_cast<unsigned>(piece_blocks + zero_blocks)),
                        dim3(kBlock), 0, st, w, s, n_tokens, E, rows, dim, static_cast<uint32_t>(slabs), scale,
-                       static_cast<uint32_t>(piece_blocks), slots, static_cast<OT*>(out), accumulate);
+                       static_cast<uint32_t>(piece_blocks), slots, out, accumulate);
     LSGD_TRY(check_launch("lsgd_embed_grad"));
     if (pieces > 1) {
         hipLaunchKernelGGL((join_pieces_kernel<kPiece, OT>), dim3(static_cast<unsigned>(ceil_div(pieces, kJoin) * slabs)),
                            dim3(kJoinThreads), 0, st, s, static_cast<uint32_t>(pieces), dim, static_cast<uint32_t>(slabs), scale,
-                           slots, static_cast<OT*>(out), accumulate);
+                           slots, out, accumulate);
         LSGD_TRY(check_launch("lsgd_embed_grad"));
     }
     return LSGD_OK;
@@ -562,10 +612,10 @@ lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint3
 
 template <typename GT, typename OT>
 lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim,
-                     float scale, float* slots, void* out, bool accumulate, hipStream_t st) {
-    return E > kRankMax
-               ? sum_rows<kManyPiece, GT, OT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st)
-               : sum_rows<kFewPiece, GT, OT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st);
+                     float scale, float* slots, OT* out, bool accumulate, hipStream_t st) {
+    return piece_of(E, dim) == kManyPiece
+               ? sum_rows_of<kManyPiece, GT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st)
+               : sum_rows_of<kFewPiece, GT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st);
 }
 
 lsgd_status check_index_type(lsgd_index_type it) {
@@ -673,17 +723,21 @@ LSGD_API lsgd_status lsgd_embed_grad(const void* const* grads, lsgd_dtype gdt, c
     char* ws = static_cast<char*>(workspace);
     Sorted s{};
     const uint32_t nt = static_cast<uint32_t>(n_tokens), e32 = static_cast<uint32_t>(E), r32 = static_cast<uint32_t>(rows);
-    if (E > 0) {
-        if (it == LSGD_I32) LSGD_TRY(sort_tokens<int32_t>(w, nt, e32, r32, l, ws, s, st));
-        else LSGD_TRY(sort_tokens<int64_t>(w, nt, e32, r32, l, ws, s, st));
-    }
     float* slots = reinterpret_cast<float*>(ws + l.slots);
     const bool acc = accumulate != 0;
-    if (gdt == LSGD_F32 && odt == LSGD_F32)
-        return sum_rows<float, float>(w, s, nt, e32, r32, dim, scale, slots, out, acc, st);
-    if (gdt == LSGD_F32) return sum_rows<float, uint16_t>(w, s, nt, e32, r32, dim, scale, slots, out, acc, st);
-    if (odt == LSGD_F32) return sum_rows<uint16_t, float>(w, s, nt, e32, r32, dim, scale, slots, out, acc, st);
-    return sum_rows<uint16_t, uint16_t>(w, s, nt, e32, r32, dim, scale, slots, out, acc, st);
+    const auto run = [&](auto grad_type, auto* o) -> lsgd_status {
+        using GT = decltype(grad_type);
+        if (E > 0) {
+            auto* zeroed = acc ? nullptr : o;
+            if (it == LSGD_I32) LSGD_TRY(sort_tokens<int32_t>(w, nt, e32, r32, dim, l, ws, s, zeroed, st));
+            else LSGD_TRY(sort_tokens<int64_t>(w, nt, e32, r32, dim, l, ws, s, zeroed, st));
+        }
+        return sum_rows<GT>(w, s, nt, e32, r32, dim, scale, slots, o, acc, st);
+    };
+    float* o32 = static_cast<float*>(out);
+    uint16_t* o16 = static_cast<uint16_t*>(out);
+    if (gdt == LSGD_F32) return odt == LSGD_F32 ? run(float{}, o32) : run(float{}, o16);
+    return odt == LSGD_F32 ? run(uint16_t{}, o32) : run(uint16_t{}, o16);
 }
 
 }  // extern "C"

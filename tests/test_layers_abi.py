@@ -89,7 +89,7 @@ def test_grad_workspace():
     f = lib.lsgd_embed_grad_workspace_size
     for workers, n, rows, dim in [(1, 1, 1, 1), (1, 4096, 1000, 64), (2, 4096, 1 << 20, 100), (128, 70, 5, 5000)]:
         assert f(workers, n, rows, dim, ctypes.byref(size)) == OK
-        assert size.value >= 8 * workers * n + 4 * rows
+        assert size.value >= 8 * workers * n
         args = dict(grads=(A,) * workers, tokens=(B,) * workers, n=n, rows=rows, dim=dim, out=1 << 44, ws=1 << 45)
         assert grad(size=size.value - 1, **args) == SIZE
     for none in ((1, 0, 5, 5), (1, 5, 0, 5), (1, 5, 5, 0)):

@@ -115,7 +115,9 @@ def zipf(n, rows, seed, dtype=torch.int64):
     (511, 24, 1400, 3, torch.int32, "zipf"), (512, 24, 2100, 2, torch.int64, "any"), (3, 520, 5000, 1, torch.int64, "same"),
     (300000, 9, 2500, 2, torch.int64, "zipf"), (70, 16, 9000, 1, torch.int32, "outside"), (2000, 1032, 3000, 4, torch.int64, "zipf"),
     (5, 8, 40000, 1, torch.int32, "any"), (40, 40, 50, 128, torch.int64, "zipf"), (90, 8, 300, 1, torch.int64, "padded"),
-    (300, 24, 6000, 2, torch.int32, "padded"), (6000, 520, 30000, 4, torch.int64, "zipf")])
+    (300, 24, 6000, 2, torch.int32, "padded"), (6000, 520, 30000, 4, torch.int64, "zipf"), (600000, 5, 3000, 1, torch.int64, "zipf"),
+    (40, 16, 8192, 1, torch.int32, "zipf"), (40, 16, 8193, 1, torch.int64, "zipf"), (9, 8, 8192, 1, torch.int64, "same"),
+    (9, 1100, 50000, 1, torch.int64, "same"), (20, 2050, 9000, 2, torch.int32, "zipf")])
 def test_grad(gdt, odt, rows, dim, n, workers, it, how):
     if how == "zipf":
         tokens = [zipf(n, rows, 10 + w, it) for w in range(workers)]
