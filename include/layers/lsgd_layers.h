@@ -83,7 +83,9 @@ LSGD_API lsgd_status lsgd_embed_lookup(const void* table, lsgd_dtype tdt, int64_
  * workspace: device memory of at least lsgd_embed_grad_workspace_size bytes,
  * 256-byte aligned; its contents are not needed between calls, and calls that
  * share one must be ordered on one stream.
- * 1 <= n_workers <= LSGD_MAX_WORKERS; n_workers * n_tokens at most 2^28, rows below 2^31.
+ * 1 <= n_workers <= LSGD_MAX_WORKERS; n_workers * n_tokens at most 2^28, rows below
+ * 2^31, dim at most 2^24. lsgd_embed_grad_workspace_size may give 0 bytes (few
+ * tokens), and workspace may then be NULL.
  * Errors as lsgd_embed_lookup.
  */
 LSGD_API lsgd_status lsgd_embed_grad_workspace_size(int32_t n_workers, int64_t n_tokens, int64_t rows,

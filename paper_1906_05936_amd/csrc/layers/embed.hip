@@ -90,6 +90,7 @@ constexpr int kSortTile = kSortThreads * kSortRounds;   // entries a workgroup o
 constexpr int kDigitBits = 9;              // two passes for tables of up to 2^18 - 1 rows
 constexpr int kBins = 1 << kDigitBits;
 constexpr int kOwnSums = 256;              // up to so many workgroups each add up the counts before its own
+constexpr int kDirectThreads = 1024, kDirectMax = 512;   // entries that need no sort of their own
 constexpr int kRankBits = 13, kRankMax = 1 << kRankBits;   // entries that are sorted by counting smaller ones
 // Sorted entries in a piece, which a wave's lanes hold: where the pieces are few,
 // latency counts and a wave takes 8 (509 entries of 203 binary32: 22 us, with 16 24,
@@ -98,6 +99,7 @@ constexpr int kRankBits = 13, kRankMax = 1 << kRankBits;   // entries that are s
 constexpr int kFewPiece = 8, kManyPiece = 32;
 constexpr int64_t kFewWaves = 1 << 14;
 int piece_of(int64_t E, int64_t dim) { return E * ceil_div(dim, 512) <= kFewWaves * kFewPiece ? kFewPiece : kManyPiece; }
+constexpr int64_t kMaxGradDim = 1 << 24;
 constexpr int64_t kMaxEntries = 1 << 28;   // grids over pieces stay within a dispatch
 
 struct Workers {
@@ -507,6 +509,128 @@ __global__ __launch_bounds__(kJoinThreads) void join_pieces_kernel(Sorted s, uin
     }
 }
 
+// The fewest entries: no sort, no workspace, one launch. A workgroup takes 64 rows of
+// the table, 512 columns. It puts the entries of its rows in order (a stable
+// counting sort by row in LDS), each of its 16 waves sums a sixteenth of them run by
+// run, and runs that reach over several waves meet in LDS, in order.
+template <typename I, typename GT, typename OT>
+__global__ __launch_bounds__(kDirectThreads) void direct_kernel(Workers w, uint32_t n_tokens, uint32_t E, uint32_t rows,
+                                                            int64_t dim, float scale, OT* __restrict__ out,
+                                                            bool accumulate) {
+    constexpr uint32_t kWaves = kDirectThreads / 64;
+    __shared__ float parts[kWaves][2][512];   // of a wave's first run and its last, where they are not whole
+    __shared__ uint32_t before[kWaves][64];   // entries of a row in the waves before
+    __shared__ uint32_t entry[kDirectMax], row_of[kDirectMax];
+    __shared__ uint32_t row_start[65];
+    __shared__ uint32_t joins[kWaves + 1];    // bit 0: a wave's first run began before, 1: it is the wave's only one
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t col = slab_column(blockIdx.y, lane);
+    const uint32_t key = threadIdx.x < E ? key_of<I>(w, threadIdx.x, n_tokens, rows) : rows;
+    const uint32_t v0 = blockIdx.x * 64;
+    const uint32_t d = key - v0;
+    const bool in = key < rows && key >= v0 && d < 64;
+    before[wave][lane] = 0;
+    __builtin_amdgcn_wave_barrier();
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 6; ++b) {
+        const uint64_t v = __ballot(d >> b & 1);
+        same &= (d >> b & 1) ? v : ~v;
+    }
+    const uint32_t ahead = __popcll(same & ((1ull << lane) - 1));
+    if (in && ahead == 0) before[wave][d] = static_cast<uint32_t>(__popcll(same));
+    __syncthreads();
+    if (wave == 0) {
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t v = 0; v < kWaves; ++v) {
+            const uint32_t c = before[v][lane];
+            before[v][lane] = n;
+            n += c;
+        }
+        uint32_t sum = n;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) {
+            const uint32_t o = __shfl_up(sum, step);
+            if (lane >= static_cast<uint32_t>(step)) sum += o;
+        }
+        row_start[lane + 1] = sum;
+        if (lane == 0) row_start[0] = 0, joins[kWaves] = 0;
+    }
+    __syncthreads();
+    const uint32_t n = row_start[64];
+    if (in) {
+        const uint32_t at = row_start[d] + before[wave][d] + ahead;
+        entry[at] = threadIdx.x;
+        row_of[at] = d;
+    }
+    __syncthreads();
+    const uint32_t each = (n + kWaves - 1) / kWaves, p = min(wave * each, n), q = min(p + each, n);
+    bool first = false, leaves = false, whole = false;
+    if (p < q) {
+        const uint32_t mine = min(p + lane, q - 1), e = entry[mine], r = row_of[mine], wk = e / n_tokens;
+        const uint64_t at = reinterpret_cast<uint64_t>(w.grads[wk]) +
+                            static_cast<uint64_t>(e - wk * n_tokens) * static_cast<uint64_t>(dim) * sizeof(GT);
+        const uint32_t lo = static_cast<uint32_t>(at), hi = static_cast<uint32_t>(at >> 32), len = q - p;
+        const uint32_t r_first = __builtin_amdgcn_readlane(r, 0), r_last = __builtin_amdgcn_readlane(r, len - 1);
+        first = p > 0 && row_of[p - 1] == r_first;
+        leaves = q < n && row_of[q] == r_last;
+        whole = r_first == r_last;
+        const uint32_t next = __shfl_down(r, 1);
+        const uint64_t ends = __ballot(lane == len - 1 || (lane < len && next != r));
+        auto row = [&](uint32_t j) {
+            // readlane gives a signed int: its low half must not be sign-extended
+            const uint32_t l = __builtin_amdgcn_readlane(lo, j), h = __builtin_amdgcn_readlane(hi, j);
+            return reinterpret_cast<const GT*>(static_cast<uint64_t>(h) << 32 | l);
+        };
+        float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        bool part = first;
+        constexpr int kAhead = 4;
+        for (uint32_t j = 0; j < len; j += kAhead) {
+            float x[kAhead][8];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) load_slab_once(row(min(j + u, len - 1)), col, dim, x[u]);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (j + u >= len) break;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[i] += x[u][i];
+                if (ends >> (j + u) & 1) {
+                    if (part || (leaves && j + u == len - 1)) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) parts[wave][part ? 0 : 1][lane + i * 64] = acc[i];
+                    } else {
+                        put_row(out + static_cast<int64_t>(v0 + __builtin_amdgcn_readlane(r, j + u)) * dim, col, dim,
+                                scale, accumulate, acc);
+                    }
+                    part = false;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+                }
+            }
+        }
+    }
+    if (lane == 0) joins[wave] = (first ? 1u : 0u) | (whole ? 2u : 0u);
+    if (!accumulate) {
+        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        const uint32_t here = min(64u, rows - v0);
+        for (uint32_t r = wave; r < here; r += kWaves)
+            if (row_start[r] == row_start[r + 1]) store_slab(out + static_cast<int64_t>(v0 + r) * dim, col, dim, zero);
+    }
+    __syncthreads();
+    if (leaves && !(first && whole)) {   // this wave's last run began in it and goes on
+        float acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = parts[wave][1][lane + i * 64];
+        for (uint32_t v = wave + 1;; ++v) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += parts[v][0][lane + i * 64];
+            if (!(joins[v] & 2) || !(joins[v + 1] & 1)) break;
+        }
+        put_row(out + static_cast<int64_t>(v0 + row_of[q - 1]) * dim, col, dim, scale, accumulate, acc);
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 struct Layout {
@@ -515,8 +639,17 @@ struct Layout {
 
 int64_t sort_blocks(int64_t E) { return ceil_div(E, kSortTile); }
 
+// Whether direct_kernel does it: up to 512 entries while its workgroups fit the card
+// at once. us, direct / sorted (rows x columns, entries): 5003 x 203, 509 14 / 21;
+// 100 x 4096, 250 13 / 20; 32000 x 1024, 510 47 / 43; 131072 x 2048, 250 128 / 112;
+// 2 x 256, 500 13 to 22 / 20, 1024 43 / 20.
+bool direct(int64_t E, int64_t rows, int64_t dim) {
+    return E <= kDirectMax && ceil_div(rows, 64) * ceil_div(dim, 512) <= 2 * device_cus();
+}
+
 Layout layout_of(int64_t E, int64_t rows, int64_t dim) {
     Layout l{};
+    if (direct(E, rows, dim)) return l;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t p = at;
@@ -618,6 +751,16 @@ lsgd_status sum_rows(const Workers& w, const Sorted& s, uint32_t n_tokens, uint3
                : sum_rows_of<kFewPiece, GT>(w, s, n_tokens, E, rows, dim, scale, slots, out, accumulate, st);
 }
 
+template <typename I, typename GT, typename OT>
+lsgd_status launch_direct(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_t rows, int64_t dim, float scale, OT* out,
+                          bool accumulate, hipStream_t st) {
+    const int64_t slabs = ceil_div(dim, 512);
+    const dim3 grid(static_cast<unsigned>(ceil_div(rows, 64)), static_cast<unsigned>(slabs));
+    hipLaunchKernelGGL((direct_kernel<I, GT, OT>), grid, dim3(kDirectThreads), 0, st, w, n_tokens, E, rows, dim, scale, out,
+                       accumulate);
+    return check_launch("lsgd_embed_grad");
+}
+
 lsgd_status check_index_type(lsgd_index_type it) {
     return it == LSGD_I32 || it == LSGD_I64 ? LSGD_OK
                                             : fail(LSGD_ERR_DTYPE, "index type %d", static_cast<int>(it));
@@ -630,7 +773,8 @@ lsgd_status check_grad_sizes(int32_t n_workers, int64_t n_tokens, int64_t rows, 
     if (n_tokens * n_workers > kMaxEntries)
         return fail(LSGD_ERR_SIZE, "n_workers * n_tokens=%lld above 2^28", static_cast<long long>(n_tokens * n_workers));
     LSGD_TRY(check_size(rows, "rows"));
-    LSGD_TRY(check_size(dim, "dim"));
+    if (dim < 0 || dim > kMaxGradDim)
+        return fail(LSGD_ERR_SIZE, "dim=%lld outside [0, 2^24]", static_cast<long long>(dim));
     LSGD_TRY(check_matrix(n_tokens * n_workers, dim, "gradients"));
     return check_matrix(rows, dim, "out");
 }
@@ -702,7 +846,7 @@ LSGD_API lsgd_status lsgd_embed_grad(const void* const* grads, lsgd_dtype gdt, c
     if (E > 0) {
         if (!grads || !tokens) return fail(LSGD_ERR_NULL, "grads or tokens is NULL");
         l = layout_of(E, rows, dim);
-        LSGD_TRY(check_buffer(workspace, 256, "workspace"));
+        if (l.bytes > 0) LSGD_TRY(check_buffer(workspace, 256, "workspace"));
         if (workspace_bytes < l.bytes)
             return fail(LSGD_ERR_SIZE, "workspace of %zu bytes, %zu needed", workspace_bytes, l.bytes);
         const int64_t isz = it == LSGD_I32 ? 4 : 8;
@@ -727,6 +871,9 @@ LSGD_API lsgd_status lsgd_embed_grad(const void* const* grads, lsgd_dtype gdt, c
     const bool acc = accumulate != 0;
     const auto run = [&](auto grad_type, auto* o) -> lsgd_status {
         using GT = decltype(grad_type);
+        if (E > 0 && direct(E, rows, dim))
+            return it == LSGD_I32 ? launch_direct<int32_t, GT>(w, nt, e32, r32, dim, scale, o, acc, st)
+                                  : launch_direct<int64_t, GT>(w, nt, e32, r32, dim, scale, o, acc, st);
         if (E > 0) {
             auto* zeroed = acc ? nullptr : o;
             if (it == LSGD_I32) LSGD_TRY(sort_tokens<int32_t>(w, nt, e32, r32, dim, l, ws, s, zeroed, st));

@@ -65,7 +65,7 @@ def test_lookup(bad, status):
     assert lookup(**bad) == status
 
 
-def grad(grads=(A,), gdt=0, tokens=(B,), it=1, workers=None, n=10, rows=100, dim=64, out=C, odt=0, acc=0, ws=D, size=MB):
+def grad(grads=(A,), gdt=0, tokens=(B,), it=1, workers=None, n=1500, rows=100, dim=64, out=C, odt=0, acc=0, ws=D, size=4 * MB):
     return lib.lsgd_embed_grad(None if grads is None else pa(grads), gdt, None if tokens is None else pa(tokens), it,
                                len(grads or ()) if workers is None else workers, n, rows, dim, 1.0, out, odt, acc, ws,
                                size, None)
@@ -74,7 +74,7 @@ def grad(grads=(A,), gdt=0, tokens=(B,), it=1, workers=None, n=10, rows=100, dim
 @pytest.mark.parametrize("bad,status", [
     (dict(gdt=3), DTYPE), (dict(odt=3), DTYPE), (dict(it=-1), DTYPE), (dict(workers=0), SIZE), (dict(workers=129), SIZE),
     (dict(n=-1), SIZE), (dict(n=BIG), SIZE), (dict(n=BIG // 2, workers=2), SIZE), (dict(rows=BIG), SIZE),
-    (dict(rows=-1), SIZE), (dict(dim=-1), SIZE), (dict(n=BIG - 1, dim=BIG - 1), SIZE), (dict(grads=None, workers=1), NULL),
+    (dict(rows=-1), SIZE), (dict(dim=-1), SIZE), (dict(dim=(1 << 24) + 1), SIZE), (dict(n=(1 << 28) + 1), SIZE), (dict(grads=None, workers=1), NULL),
     (dict(tokens=None), NULL), (dict(grads=(None,)), NULL), (dict(tokens=(None,)), NULL), (dict(out=None), NULL),
     (dict(ws=None), NULL), (dict(ws=D + 128), ALIGN), (dict(grads=(A + 8,)), ALIGN), (dict(tokens=(B + 4,)), ALIGN),
     (dict(out=C + 8), ALIGN), (dict(size=16), SIZE), (dict(out=A), ALIAS), (dict(ws=A), ALIAS), (dict(ws=B), ALIAS),
@@ -87,12 +87,12 @@ def test_grad(bad, status):
 def test_grad_workspace():
     size = ctypes.c_size_t()
     f = lib.lsgd_embed_grad_workspace_size
-    for workers, n, rows, dim in [(1, 1, 1, 1), (1, 4096, 1000, 64), (2, 4096, 1 << 20, 100), (128, 70, 5, 5000)]:
+    for workers, n, rows, dim in [(1, 513, 1, 1), (1, 5, 1 << 20, 64), (1, 4096, 1000, 64), (2, 4096, 1 << 20, 100), (128, 70, 5, 5000)]:
         assert f(workers, n, rows, dim, ctypes.byref(size)) == OK
         assert size.value >= 8 * workers * n
         args = dict(grads=(A,) * workers, tokens=(B,) * workers, n=n, rows=rows, dim=dim, out=1 << 44, ws=1 << 45)
         assert grad(size=size.value - 1, **args) == SIZE
-    for none in ((1, 0, 5, 5), (1, 5, 0, 5), (1, 5, 5, 0)):
+    for none in ((1, 0, 5, 5), (1, 5, 0, 5), (1, 5, 5, 0), (1, 512, 5, 5), (4, 128, 5, 5)):
         assert f(*none, ctypes.byref(size)) == OK and size.value == 0
     assert f(0, 1, 1, 1, ctypes.byref(size)) == SIZE and f(1, 1, 1, 1, None) == NULL
 

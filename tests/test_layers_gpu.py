@@ -117,7 +117,8 @@ def zipf(n, rows, seed, dtype=torch.int64):
     (5, 8, 40000, 1, torch.int32, "any"), (40, 40, 50, 128, torch.int64, "zipf"), (90, 8, 300, 1, torch.int64, "padded"),
     (300, 24, 6000, 2, torch.int32, "padded"), (6000, 520, 30000, 4, torch.int64, "zipf"), (600000, 5, 3000, 1, torch.int64, "zipf"),
     (40, 16, 8192, 1, torch.int32, "zipf"), (40, 16, 8193, 1, torch.int64, "zipf"), (9, 8, 8192, 1, torch.int64, "same"),
-    (9, 1100, 50000, 1, torch.int64, "same"), (20, 2050, 9000, 2, torch.int32, "zipf")])
+    (9, 1100, 50000, 1, torch.int64, "same"), (200, 520, 512, 1, torch.int64, "zipf"), (64, 40, 512, 1, torch.int32, "same"),
+    (130, 9, 513, 1, torch.int64, "zipf"), (40000, 600, 500, 1, torch.int64, "zipf"), (65, 24, 170, 3, torch.int64, "any"), (3, 16, 500, 1, torch.int64, "zipf"), (20, 2050, 9000, 2, torch.int32, "zipf")])
 def test_grad(gdt, odt, rows, dim, n, workers, it, how):
     if how == "zipf":
         tokens = [zipf(n, rows, 10 + w, it) for w in range(workers)]
@@ -634,6 +635,7 @@ def refused():
     x, t = randn(8, 16, seed=1), torch.zeros(8, dtype=torch.int64, device=DEV)
     (q, s), (w, ws) = lsgd.empty8(8, 16), lsgd.empty8(4, 16, 128)
     g = x[:, :4].bfloat16().contiguous()
+    big, many = randn(3000, 16, seed=2), torch.zeros(3000, dtype=torch.int64, device=DEV)
     return [
         (TypeError, lambda: lsgd.embed_lookup(x.half(), t, x)),
         (TypeError, lambda: lsgd.embed_lookup(x, t.short(), x)),
@@ -646,7 +648,8 @@ def refused():
         (TypeError, lambda: lsgd.embed_grad([x, x], [t, t.int()], x.clone())),
         (TypeError, lambda: lsgd.embed_grad([x, x.bfloat16()], [t, t], x.clone())),
         (lsgd.LsgdError, lambda: lsgd.embed_grad([x], [t], x)),
-        (lsgd.LsgdError, lambda: lsgd.embed_grad([x], [t], x.clone(), workspace=torch.empty(1, dtype=torch.uint8, device=DEV))),
+        (lsgd.LsgdError, lambda: lsgd.embed_grad([x] * 150, [t] * 128 + [t] * 22, x.clone())),
+        (lsgd.LsgdError, lambda: lsgd.embed_grad([big], [many], x.clone(), workspace=torch.empty(1, dtype=torch.uint8, device=DEV))),
         (ValueError, lambda: lsgd.quant8(x, q[:7], s)),
         (TypeError, lambda: lsgd.quant8(x, q.view(torch.int8), s)),
         (TypeError, lambda: lsgd.quant8(x.double(), q, s)),
@@ -662,7 +665,7 @@ def refused():
     ]
 
 
-@pytest.mark.parametrize("k", range(24))
+@pytest.mark.parametrize("k", range(25))
 def test_refusals_agree(k, monkeypatch):
     from paper_1906_05936_amd import _lib
     kind, call = refused()[k]
