@@ -114,7 +114,8 @@ LSGD_API lsgd_status lsgd_quant8(const void* x, lsgd_dtype xdt, int64_t rows, in
  * one of the n_transposed copies those of its transpose (cols x rows: codes of
  * pitch lsgd_pitch8(rows)), which the gradient of a layer's input needs. The
  * arrays are host arrays of device pointers (NULL for a count of 0). Counts in
- * [0, LSGD_MAX_REPLICAS]. No-op where rows or cols is 0, or both counts are.
+ * [0, LSGD_MAX_REPLICAS]; rows at most 65535 * 128. No-op where rows or cols is 0,
+ * or both counts are.
  * Errors as lsgd_embed_lookup.
  */
 LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t cols,

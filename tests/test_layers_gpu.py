@@ -370,20 +370,20 @@ def check_product(m, n, k, ablock, bblock, odt, seed=0, spread=2.0):
 @pytest.mark.parametrize("m,n,k", [
     (1, 1, 1), (1, 16, 128), (2, 17, 129), (16, 128, 512), (17, 130, 640), (33, 1000, 777), (64, 64, 4096),
     (65, 48, 300), (127, 129, 1024), (128, 128, 128), (129, 257, 257), (200, 520, 1537), (256, 256, 256),
-    (300, 1025, 520), (513, 700, 640), (1100, 2050, 384)])
+    (300, 1025, 520), (513, 700, 640), (1100, 2050, 384), (2100, 4001, 300), (2304, 4100, 1152), (4097, 2090, 200), (2050, 4097, 90)])
 def test_matmul8(odt, m, n, k):
     check_product(m, n, k, 1, 128, odt, seed=m + n + k)
 
 
 @pytest.mark.parametrize("odt", [F32, BF16])
 @pytest.mark.parametrize("ablock,bblock", [(1, 1), (128, 1), (128, 128)])
-@pytest.mark.parametrize("m,n,k", [(5, 300, 200), (300, 260, 515), (1, 2, 130)])
+@pytest.mark.parametrize("m,n,k", [(5, 300, 200), (300, 260, 515), (1, 2, 130), (1000, 1300, 260), (2150, 4010, 260)])
 def test_matmul8_blocks(odt, ablock, bblock, m, n, k):
     check_product(m, n, k, ablock, bblock, odt, seed=3)
 
 
 @pytest.mark.parametrize("odt", [F32, BF16])
-@pytest.mark.parametrize("m,n,k", [(3, 20, 300), (150, 140, 300), (600, 600, 140)])
+@pytest.mark.parametrize("m,n,k", [(3, 20, 300), (150, 140, 300), (600, 600, 140), (1200, 2100, 300), (2200, 4003, 300)])
 def test_matmul8_whole_numbers_and_their_places(odt, m, n, k):
     """Whole numbers of up to 3: every product and sum is exact in both forms
     (bfloat16 outputs: sums below 256), so each output has one right value."""
@@ -411,7 +411,7 @@ def test_matmul8_scales_at_their_ends(odt):
 
 
 @pytest.mark.parametrize("odt", [F32, BF16])
-@pytest.mark.parametrize("m,n", [(10, 30), (300, 400)])
+@pytest.mark.parametrize("m,n", [(10, 30), (300, 400), (1100, 2000), (2100, 4001)])
 def test_matmul8_nan_stays_in_its_row_and_column(odt, m, n):
     a, b = randn(m, 300, seed=1), randn(n, 300, seed=2)
     a[m - 1, 150], b[3, 299] = float("nan"), float("inf")
@@ -568,6 +568,66 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for key in ("x", "y", "dw", "dtable"):
             assert torch.equal(graphed[key], eager[key]), (seed, key)
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams with workspaces of their own, in flight together."""
+    n, rows, dim = 20000, 500, 256
+    tokens, g = [zipf(n, rows, s) for s in (1, 2)], [randn(n, dim, seed=s) for s in (3, 4)]
+    x, dy = [as8(randn(n, dim, seed=s), 1) for s in (5, 6)], [randn(n, 96, seed=s, dtype=BF16) for s in (7, 8)]
+    alone = [(nans(rows, dim), nans(96, dim)) for _ in range(2)]
+    for s in range(2):
+        lsgd.embed_grad([g[s]], [tokens[s]], alone[s][0])
+        lsgd.weight_grad8(dy[s], *x[s], alone[s][1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        both = [(nans(rows, dim), nans(96, dim)) for _ in range(2)]
+        torch.cuda.synchronize()
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                lsgd.embed_grad([g[s]], [tokens[s]], both[s][0])
+                lsgd.weight_grad8(dy[s], *x[s], both[s][1])
+        torch.cuda.synchronize()
+        for s in range(2):
+            assert torch.equal(both[s][0], alone[s][0]) and torch.equal(both[s][1], alone[s][1])
+
+
+def test_one_graph_allocates_its_workspaces():
+    """Captured without workspaces of the caller's: they live in the graph's own
+    memory, so that two graphs replayed in turn keep apart."""
+    n, rows, dim = 9000, 300, 64
+    tokens, g = [zipf(n, rows, s) for s in (1, 2)], [randn(n, dim, seed=s) for s in (3, 4)]
+    want, out, graphs = [nans(rows, dim) for _ in range(2)], [nans(rows, dim) for _ in range(2)], []
+    for s in range(2):
+        lsgd.embed_grad([g[s]], [tokens[s]], want[s])
+    torch.cuda.synchronize()
+    for s in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[s]):
+            lsgd.embed_grad([g[s]], [tokens[s]], out[s])
+    for _ in range(3):
+        for s in range(2):
+            out[s].fill_(float("nan"))
+            graphs[s].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_offsets_past_32_bits():
+    """A table and its gradient of more than 2^32 elements."""
+    rows, dim = (1 << 22) + 3, 1032
+    table = torch.zeros(rows, dim, device=DEV, dtype=BF16)
+    tokens = torch.tensor([rows - 1, 0, rows - 2, rows - 1], device=DEV)
+    table[rows - 1], table[rows - 2], table[0] = 3.0, 2.0, 1.0
+    out = nans(4, dim)
+    lsgd.embed_lookup(table, tokens, out)
+    assert torch.equal(out[:, 0].cpu(), torch.tensor([3.0, 1.0, 2.0, 3.0])) and torch.equal(out, out[:, :1].expand(-1, dim))
+    g = torch.arange(4, device=DEV, dtype=F32).view(4, 1).expand(4, dim).contiguous() + 1
+    table.fill_(7.0)
+    lsgd.embed_grad([g], [tokens], table)
+    assert (table[rows - 1] == 5).all() and (table[0] == 2).all() and (table[rows - 2] == 3).all()
+    assert torch.count_nonzero(table[1:rows - 2]) == 0
 
 
 def test_on_a_stream_of_its_own():
