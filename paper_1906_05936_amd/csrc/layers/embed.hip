@@ -50,8 +50,9 @@ __global__ __launch_bounds__(kBlock) void embed_lookup_kernel(const TT* __restri
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * per + threadIdx.x / lanes; i < n_tokens;
          i += static_cast<int64_t>(gridDim.x) * per) {
         const int64_t t = token_row(tokens, i, rows);
+        const float f = t >= 0 ? scale : 0.0f;
         for (int64_t c = threadIdx.x % lanes * kVec; c < dim; c += lanes * kVec)
-            scaled_copy(t >= 0 ? table + t * dim + c : nullptr, scale, out + i * dim + c,
+            scaled_copy(t >= 0 ? table + t * dim + c : nullptr, f, out + i * dim + c,
                         static_cast<int>(min(dim - c, static_cast<int64_t>(kVec))));
     }
 }
