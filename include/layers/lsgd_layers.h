@@ -28,7 +28,7 @@
  * rounded to the nearest code, ties to the even one; NaN and infinities become
  * NaN. (A power of two costs a floating format no relative precision, is
  * divided by and multiplied with exactly, and makes a transposed copy hold the
- * same numbers.)
+ * same numbers.) Scales made elsewhere may be bytes 1 to 254.
  *
  * The conventions of lsgd.h hold (memory, streams, validation, aliasing,
  * errors; every matrix is contiguous, row-major): buffers are 16-byte aligned,

@@ -394,6 +394,7 @@ __global__ __launch_bounds__(kBlock) void add_parts_kernel(const float* __restri
 
 // How a call is done: tiles of 256, 128 or 64 outputs each way, and the summed rows
 // in `count` shares whose parts are added at the end.
+constexpr int64_t kMaxSplit = int64_t{1} << 30;   // outputs: add_parts_kernel's threads stay within a dispatch
 struct Way {
     int tile, count;
     int64_t share;
@@ -414,7 +415,8 @@ Way way_of(int64_t m, int64_t n, int64_t k) {
         if (tile == 256 && (n < 256 || pitch8(k) < 256)) continue;
         const int64_t tiles = ceil_div(n, tile) * ceil_div(k, tile), at_once = device_cus() * (tile == 256 ? 1 : tile == 128 ? 2 : 4);
         const double stage_us = tile == 256 ? 1.7 : 1.2, fixed_us = tile == 256 ? 8 : tile == 128 ? 4 : 3;
-        for (int64_t count = 1; count <= std::min<int64_t>(stages, 64); ++count) {
+        const int64_t most = n * k > kMaxSplit ? 1 : std::min<int64_t>(stages, 64);
+        for (int64_t count = 1; count <= most; ++count) {
             const int64_t each = ceil_div(stages, count);
             if (count > 1 && ceil_div(stages, each) != count) continue;
             const double us = ceil_div(tiles * count, at_once) * (each * stage_us + fixed_us) +
