@@ -89,9 +89,9 @@ def _workspace(size_of, sizes, workspace, stream, device):
     if workspace is not None:
         _dev_tensor(workspace, "workspace", torch.uint8, None, device)
     elif n.value:
-        workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
-        if stream is not None:   # freed here, used there
-            workspace.record_stream(stream)
+        # on the call's stream: memory freed on another may still be read there
+        with torch.cuda.stream(stream):
+            workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
     else:
         return None, 0, None
     return workspace.data_ptr(), workspace.numel(), workspace

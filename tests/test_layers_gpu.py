@@ -77,6 +77,15 @@ def test_lookup_non_finite_rows_and_extreme_tokens():
     assert torch.count_nonzero(out[2:5]) == 0
 
 
+@pytest.mark.parametrize("odt", [F32, BF16])
+def test_lookup_outside_the_table_is_zero_whatever_the_scale(odt):
+    table, tokens = randn(3, 21, seed=1), torch.tensor([-1, 2, 3], device=DEV)
+    for scale in (float("inf"), float("nan"), -2.0):
+        out = nans(3, 21, dtype=odt)
+        lsgd.embed_lookup(table, tokens, out, scale)
+        assert (out[::2] == 0).all()
+
+
 def test_lookup_empty():
     out = nans(0, 8)
     lsgd.embed_lookup(randn(3, 8), torch.empty(0, dtype=torch.int64, device=DEV), out)
@@ -299,6 +308,20 @@ def test_quant8_extreme_values(dtype):
     lsgd.quant8(x, codes, scales)
     check_8bit(x, codes, scales, 1)
     guard()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_quant8_passes_over_signalling_nans(dtype):
+    """The block's scale is that of its finite elements, wherever the NaN stands."""
+    whole = torch.int32 if dtype == F32 else torch.int16
+    signalling = torch.tensor(0x7f800001 if dtype == F32 else 0x7f81, dtype=whole, device=DEV).view(dtype)
+    for at in (0, 7, 64, 127):
+        x = torch.full((2, 128), 3.0, device=DEV, dtype=dtype)
+        x.view(whole)[0, at] = signalling.view(whole)
+        codes, scales = lsgd.empty8(2, 128)
+        lsgd.quant8(x, codes, scales)
+        assert torch.equal(scales[0, :1].view(torch.uint8), scales[1, :1].view(torch.uint8))
+        assert torch.isnan(codes.float()[0, at]) and torch.isnan(codes.float()).sum() == 1
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (127, 3), (128, 128), (129, 257), (300, 1000), (1025, 130), (5, 700)])
@@ -628,6 +651,101 @@ def test_offsets_past_32_bits():
     lsgd.embed_grad([g], [tokens], table)
     assert (table[rows - 1] == 5).all() and (table[0] == 2).all() and (table[rows - 2] == 3).all()
     assert torch.count_nonzero(table[1:rows - 2]) == 0
+
+
+def test_activations_past_32_bits():
+    """8 bits of more than 2^32 elements: the last rows as of themselves alone."""
+    rows, cols = (1 << 20) + 77, 4097
+    x = torch.zeros(rows, cols, device=DEV, dtype=BF16)
+    x[-300:], x[:5] = randn(300, cols, seed=1), randn(5, cols, seed=2)
+    codes, scales = as8(x, 1)
+    for part in (slice(rows - 300, rows), slice(0, 5)):
+        q, s = as8(x[part].clone(), 1)
+        assert torch.equal(codes[part].view(torch.uint8), q.view(torch.uint8))
+        assert torch.equal(scales[part].view(torch.uint8), s.view(torch.uint8))
+    # and products and gradients of them, whose other rows count as 0
+    w, last = as8(randn(130, cols, seed=3), 1), (codes[-300:].contiguous(), scales[-300:].contiguous())
+    x64, w64 = values(*last, 1, cols), values(*w, 1, cols)
+    want, size = x64 @ w64.t().contiguous(), x64.abs() @ w64.abs().t().contiguous()
+    for odt in (F32, BF16):
+        out = nans(rows, 130, dtype=odt)
+        lsgd.matmul8(codes, scales, *w, out)
+        bound = size * 2.0 ** -10 * 1.01 + want.abs() * HALF[BF16] * 1.01 if odt == BF16 else size * cols * U32
+        assert_close(out[-300:], want, bound)
+        assert torch.count_nonzero(out[5:-300]) == 0
+    g = torch.zeros(rows, 66, device=DEV, dtype=BF16)
+    g[-300:] = randn(300, 66, seed=4)
+    out, g64 = nans(66, cols), g[-300:].double().t().contiguous()
+    lsgd.weight_grad8(g, codes, scales, out)
+    assert_close(out, g64 @ x64, (g64.abs() @ x64.abs()) * (300 * U32))
+
+
+def test_outputs_past_32_bits():
+    """Products and parameter gradients of more than 2^32 elements."""
+    m, n, k = 65536 + 130, 65536 + 3, 256
+    a, b = as8(randn(m, k, seed=1), 1), as8(randn(n, k, seed=2), 1)
+    out = nans(m, n, dtype=BF16)
+    lsgd.matmul8(*a, *b, out)
+    a64, b64 = values(*a, 1, k), values(*b, 1, k)
+    for i in (0, 32768, m - 1):
+        want, size = b64 @ a64[i], b64.abs() @ a64[i].abs()
+        assert_close(out[i], want, size * 2.0 ** -10 * 1.01 + want.abs() * HALF[BF16] * 1.01)
+    assert not torch.isnan(out).any()
+    del out, a, b
+    g, x = randn(256, m, seed=3, dtype=BF16), as8(randn(256, n, seed=4), 1)
+    out = nans(m, n, dtype=BF16)
+    lsgd.weight_grad8(g, *x, out)
+    x64 = values(*x, 1, n)
+    for i in (0, 32768, m - 1):
+        gi = g[:, i].double()
+        want, size = gi @ x64, gi.abs() @ x64.abs()
+        assert_close(out[i], want, size * 256 * U32 + want.abs() * HALF[BF16] * (1 + U32))
+    assert not torch.isnan(out).any()
+
+
+def test_copies_past_32_bits():
+    rows, cols = (1 << 22) + 200, 1025
+    p = torch.zeros(rows, cols, device=DEV)
+    p[-256:] = randn(256, cols, seed=1)
+    first = rows // 128 * 128 - 128   # the last whole block of rows, and what is behind it
+    copies = [lsgd.empty8(rows, cols, 128), lsgd.empty8(cols, rows, 128)]
+    lsgd.copy_out8(p, [copies[0]], [copies[1]])
+    q, s = lsgd.empty8(rows - first, cols, 128)
+    lsgd.copy_out8(p[first:].contiguous(), [(q, s)])
+    assert torch.equal(copies[0][0][first:].view(torch.uint8), q.view(torch.uint8))
+    assert torch.equal(copies[0][1][first // 128:].view(torch.uint8), s.view(torch.uint8))
+    assert torch.equal(copies[1][0][:, first:rows].view(torch.uint8), q.view(torch.uint8)[:, :cols].T)
+
+
+@pytest.mark.parametrize("name", ["gradient", "weights"])
+def test_a_workspace_for_another_stream(name):
+    """`stream` names a stream that is not the current one: the workspace that the call
+    allocates is not memory that work of the current stream still reads."""
+    n, rows, dim = 9000, 300, 64
+    side = torch.cuda.Stream()
+    if name == "gradient":
+        size = lsgd.embed_grad_workspace_size(1, n, rows, dim)
+        g, t, out = randn(n, dim, seed=1), zipf(n, rows, 2), nans(rows, dim)
+        call = lambda **kw: lsgd.embed_grad([g], [t], out, **kw)
+    else:
+        size = lsgd.weight_grad8_workspace_size(n, 64, 64)
+        g, x, out = randn(n, 64, seed=1, dtype=BF16), as8(randn(n, 64, seed=2), 1), nans(64, 64)
+        call = lambda **kw: lsgd.weight_grad8(g, *x, out, **kw)
+    assert size > 0
+    call()
+    want = out.clone()
+    out.fill_(float("nan"))
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    held = torch.full((size,), 1, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)
+    seen = held.clone()
+    del held
+    call(stream=side)
+    side.synchronize()
+    torch.cuda.synchronize()
+    assert (seen == 1).all() and torch.equal(out, want)
 
 
 def test_on_a_stream_of_its_own():
