@@ -201,7 +201,8 @@ __global__ __launch_bounds__(256) void weight_grad8_kernel(const uint16_t* __res
 // bfloat16 on their way from there. (Loads straight into LDS have to have arrived
 // before the next transposing read, which took a third longer.) Needs 256 rows and
 // columns. The last tile of a row or column of tiles lies inside the matrix too and
-// stores what no other tile does.
+// stores what no other tile does. (So a row of the last tile ends with a whole word,
+// also for an odd n, and add_last has nothing to add.)
 constexpr int kWideTile = 256;
 
 template <typename OT>
@@ -358,9 +359,8 @@ __global__ __launch_bounds__(256) void weight_grad8_wide_kernel(const uint16_t* 
         for (int q = 0; q < 16; ++q) {
             const int r = q * 2 + lane / 32;
             const int64_t row = n0 + wn + i * 32 + r;
-            f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * 512 + ((lane % 32) ^ r) * 16);
+            const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * 512 + ((lane % 32) ^ r) * 16);
             if (row < first_n || left <= 0) continue;
-            if (n % 2 && m > 0 && row == n - 1 && end == m) add_last(v, grad, x, scales, m, n, pitch, spitch, col);
             put4(part, out, row * k + col, left, v, accumulate);
         }
         __builtin_amdgcn_wave_barrier();

@@ -459,7 +459,9 @@ def test_matmul8_empty():
 @pytest.mark.parametrize("odt", [F32, BF16])
 @pytest.mark.parametrize("m,n,k", [
     (1, 1, 1), (2, 3, 5), (63, 16, 128), (64, 128, 128), (65, 129, 130), (500, 7, 1000), (1000, 300, 77), (4099, 40, 260),
-    (257, 513, 640), (129, 1000, 1025), (3001, 256, 256), (64, 9, 140), (2050, 1021, 2000), (4097, 2047, 1100), (300, 4100, 4300)])
+    (257, 513, 640), (129, 1000, 1025), (3001, 256, 256), (64, 9, 140), (2050, 1021, 2000), (4097, 2047, 1100), (300, 4100, 4300),
+    (700, 5001, 4999), (2500, 4096, 4096), (3001, 2051, 4001), (1, 8001, 8000), (8666, 1537, 2900),
+    (11999, 2047, 1290)])
 def test_weight_grad8(odt, m, n, k):
     x = randn(m, k, seed=m) * torch.exp(randn(m, k, seed=n))
     g = randn(m, n, seed=k, dtype=BF16)
