@@ -127,7 +127,8 @@ def zipf(n, rows, seed, dtype=torch.int64):
     (300, 24, 6000, 2, torch.int32, "padded"), (6000, 520, 30000, 4, torch.int64, "zipf"), (600000, 5, 3000, 1, torch.int64, "zipf"),
     (40, 16, 8192, 1, torch.int32, "zipf"), (40, 16, 8193, 1, torch.int64, "zipf"), (9, 8, 8192, 1, torch.int64, "same"),
     (9, 1100, 50000, 1, torch.int64, "same"), (200, 520, 512, 1, torch.int64, "zipf"), (64, 40, 512, 1, torch.int32, "same"),
-    (130, 9, 513, 1, torch.int64, "zipf"), (40000, 600, 500, 1, torch.int64, "zipf"), (65, 24, 170, 3, torch.int64, "any"), (3, 16, 500, 1, torch.int64, "zipf"), (20, 2050, 9000, 2, torch.int32, "zipf")])
+    (130, 9, 513, 1, torch.int64, "zipf"), (40000, 600, 500, 1, torch.int64, "zipf"), (65, 24, 170, 3, torch.int64, "any"), (3, 16, 500, 1, torch.int64, "zipf"), (20, 2050, 9000, 2, torch.int32, "zipf"),
+    (300000, 9, 9000, 2, torch.int64, "any"), (1000, 4, 1100000, 1, torch.int64, "zipf"), (300000, 12, 600000, 2, torch.int32, "zipf")])
 def test_grad(gdt, odt, rows, dim, n, workers, it, how):
     if how == "zipf":
         tokens = [zipf(n, rows, 10 + w, it) for w in range(workers)]
@@ -393,7 +394,8 @@ def check_product(m, n, k, ablock, bblock, odt, seed=0, spread=2.0):
 @pytest.mark.parametrize("m,n,k", [
     (1, 1, 1), (1, 16, 128), (2, 17, 129), (16, 128, 512), (17, 130, 640), (33, 1000, 777), (64, 64, 4096),
     (65, 48, 300), (127, 129, 1024), (128, 128, 128), (129, 257, 257), (200, 520, 1537), (256, 256, 256),
-    (300, 1025, 520), (513, 700, 640), (1100, 2050, 384), (2100, 4001, 300), (2304, 4100, 1152), (4097, 2090, 200), (2050, 4097, 90)])
+    (300, 1025, 520), (513, 700, 640), (1100, 2050, 384), (2100, 4001, 300), (2304, 4100, 1152), (4097, 2090, 200), (2050, 4097, 90),
+    (500, 510, 200), (1000, 1023, 400), (1024, 1000, 130), (6200, 8200, 300)])
 def test_matmul8(odt, m, n, k):
     check_product(m, n, k, 1, 128, odt, seed=m + n + k)
 
@@ -637,6 +639,16 @@ def test_one_graph_allocates_its_workspaces():
             graphs[s].replay()
         torch.cuda.synchronize()
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_lookup_of_more_rows_than_workgroups():
+    n, dim = (1 << 24) + 5, 1025
+    tokens = randint(n, 0, 3, seed=1, dtype=torch.int32)
+    table, out = randn(3, dim, seed=2, dtype=BF16), nans(n, dim, dtype=BF16)
+    lsgd.embed_lookup(table, tokens, out)
+    for part in (slice(0, 100), slice(n - 100, n), slice(n // 2, n // 2 + 100)):
+        assert torch.equal(out[part], table[tokens[part].long()])
+    assert torch.equal(out[:, dim - 1], table[tokens.long(), dim - 1])
 
 
 def test_offsets_past_32_bits():
