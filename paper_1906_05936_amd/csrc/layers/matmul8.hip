@@ -16,8 +16,9 @@ struct Operand {
 // A workgroup of WM x WN waves computes a tile of (WM * TM * 16) x (WN * TN *
 // 16) outputs, 128 columns of a and b at a time, which the next step's loads
 // (straight into LDS, no registers) overlap. LDS rows are 128 bytes, their
-// 16-byte chunks exchanged by row % 8, so that the 8 rows of a fragment read
-// meet all banks. b is the matrix instruction's first operand: a lane then holds
+// 16-byte chunks exchanged by row / 2 % 8, so that the same chunk of 16 rows lies in
+// all 64 banks (by row % 8 two rows of 16 met in each bank, and the kernel below
+// took 215 us instead of 209). b is the matrix instruction's first operand: a lane then holds
 // 4 neighbouring columns of one output row. Offsets inside a tile are 32-bit.
 template <int TM, int TN, int WM, int WN, bool Exact, typename OT>
 __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
@@ -25,6 +26,7 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
     constexpr int kWaves = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, kStage = (BM + BN) * 128;
     constexpr int kLoadsA = BM / 8 / kWaves, kLoads = (BM + BN) / 8 / kWaves;   // of 8 rows each, per wave
     static_assert(kLoadsA * 8 * kWaves == BM && kLoads * 8 * kWaves == BM + BN, "every wave loads as many rows");
+    static_assert(kWaves % 2 == 0, "row / 2 % 8 of a loaded row");
     __shared__ __align__(16) uint8_t lds[2 * kStage];
     uint32_t tm, tn;
     if (!order.tile(blockIdx.x, tm, tn)) return;
@@ -41,7 +43,7 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
         const uint32_t row = ((i < kLoadsA ? i : i - kLoadsA) * kWaves + wave) * 8 + lane / 8;
-        from[i] = min(row, i < kLoadsA ? last_a : last_b) * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+        from[i] = min(row, i < kLoadsA ? last_a : last_b) * pitch + ((lane % 8) ^ (wave % 2 * 4 + lane / 16)) * 16;
     }
     auto fetch = [&](uint8_t* stage) {
 #pragma unroll
@@ -62,8 +64,8 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
     uint32_t wa[TM], wb[TN];
-    // fragment rows: lane % 16, whose row % 8 exchanges the chunks
-    const int at = lane % 16 * 128 + ((lane / 16) ^ (lane % 8)) * 16;
+    // fragment rows: lane % 16, whose row / 2 exchanges the chunks
+    const int at = lane % 16 * 128 + ((lane / 16) ^ (lane / 2 % 8)) * 16;
     const int at_a = wm * 128 + at, at_b = (BM + wn) * 128 + at;
     fetch(lds);
     for (int base = 0; base < steps; base += 4) {
@@ -120,7 +122,9 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 // columns of a and b) is in LDS for the fragment reads while the next one
 // arrives. A workgroup goes through several tiles, and its loads run two
 // stages ahead, across the end of a tile: the next one's first stages arrive
-// while this one's outputs leave.
+// while this one's outputs leave. 8192 x 8192 x 4096: 209 to 217 us, 2.5 to 2.6
+// PFLOP/s; the matrix units are busy for two thirds of the cycles, at a clock that
+// the power they take brings down to 1.9 GHz.
 constexpr int kWideTile = 256;
 
 // The stage that a workgroup loads next: tile, place in it, addresses. The last
@@ -129,43 +133,46 @@ constexpr int kWideTile = 256;
 struct WideLoads {
     static constexpr int kLoads = 8;          // of 8 rows each, per wave and operand
     static constexpr int kStage = 2 * kWideTile * 128;
-    uint32_t row_a[4], row_b[4];              // scale rows of a wave's fragments
-    Buffer codes_a, codes_b;
-    const uint8_t *scales_a, *scales_b;
+    uint32_t row_a[2], row_b[2];              // scale rows of two of a wave's fragments each
+    Buffer codes_a, codes_b, scales_a, scales_b;
     uint32_t stage;
 
     static __device__ __forceinline__ int64_t origin(uint32_t tile, int64_t rows) {
         return min(static_cast<int64_t>(tile) * kWideTile, rows - kWideTile);
     }
-    __device__ __forceinline__ WideLoads() : codes_a(nullptr, 0), codes_b(nullptr, 0) {}
+    __device__ __forceinline__ WideLoads() : codes_a(nullptr, 0), codes_b(nullptr, 0), scales_a(nullptr, 0), scales_b(nullptr, 0) {}
     __device__ __forceinline__ void set(const Operand& A, const Operand& B, uint32_t tm, uint32_t tn, uint32_t pitch,
                                         uint32_t spitch, int wave, int lane) {
         const int64_t m0 = origin(tm, A.rows), n0 = origin(tn, B.rows);
         codes_a = Buffer(A.codes + m0 * pitch, kWideTile * pitch);
         codes_b = Buffer(B.codes + n0 * pitch, kWideTile * pitch);
-        scales_a = A.scales + (m0 >> A.shift) * spitch;
-        scales_b = B.scales + (n0 >> B.shift) * spitch;
         const uint32_t part_a = static_cast<uint32_t>(m0) & ((1u << A.shift) - 1);
         const uint32_t part_b = static_cast<uint32_t>(n0) & ((1u << B.shift) - 1);
+        scales_a = Buffer(A.scales + (m0 >> A.shift) * spitch, (((part_a + kWideTile - 1) >> A.shift) + 1) * spitch);
+        scales_b = Buffer(B.scales + (n0 >> B.shift) * spitch, (((part_b + kWideTile - 1) >> B.shift) + 1) * spitch);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            row_a[i] = ((part_a + wave % 2 * 128 + i * 32 + lane % 32) >> A.shift) * spitch;
-            row_b[i] = ((part_b + wave / 2 * 128 + i * 32 + lane % 32) >> B.shift) * spitch;
+        for (int i = 0; i < 2; ++i) {
+            row_a[i] = ((part_a + wave % 2 * 128 + i * 64 + lane) >> A.shift) * spitch;
+            row_b[i] = ((part_b + wave / 2 * 128 + i * 64 + lane) >> B.shift) * spitch;
         }
         stage = 0;
     }
-    // `from`: a lane's 16 bytes of the wave's first 8 rows
-    __device__ __forceinline__ void fetch(uint8_t* to, uint32_t from, uint32_t pitch, int wave) const {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            codes_a.load_lds16(from, stage * 128 + i * 32 * pitch, to + (i * 4 + wave) * 1024);
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            codes_b.load_lds16(from, stage * 128 + i * 32 * pitch, to + (kWideTile / 8 + i * 4 + wave) * 1024);
+    // The q-th of a stage's 2 kLoads loads; `from`: a lane's 16 bytes of the wave's first 8 rows.
+    __device__ __forceinline__ void fetch(int q, uint8_t* to, uint32_t from, uint32_t pitch, int wave) const {
+        (q < kLoads ? codes_a : codes_b).load_lds16(from, stage * 128 + q % kLoads * 32 * pitch, to + (q * 4 + wave) * 1024);
     }
-    __device__ __forceinline__ void fetch_scales(uint32_t (&a)[4], uint32_t (&b)[4]) const {
+    // A word holds a row's scales of four stages. It is loaded for the first of them;
+    // for the others the offsets lie outside the buffer, which costs no access (a byte a
+    // stage, for 32 rows at a time: 230 us instead of 215).
+    __device__ __forceinline__ bool first_of_four() const { return stage % 4 == 0; }
+    __device__ __forceinline__ void fetch_scales(int i, uint32_t (&words)[4]) const {
+        words[i] = (i < 2 ? scales_a : scales_b).load4((i < 2 ? row_a[i] : row_b[i - 2]) | (first_of_four() ? 0 : 0x80000000u), stage);
+    }
+    __device__ __forceinline__ void fetch_all(uint8_t* to, uint32_t from, uint32_t pitch, int wave, uint32_t (&words)[4]) const {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = scales_a[row_a[i] + stage], b[i] = scales_b[row_b[i] + stage];
+        for (int i = 0; i < 4; ++i) fetch_scales(i, words);
+#pragma unroll
+        for (int q = 0; q < 2 * kLoads; ++q) fetch(q, to, from, pitch, wave);
     }
 };
 
@@ -178,37 +185,37 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
     const uint32_t stages = pitch / 128;
     uint32_t tm, tn, next_tm, next_tn, block = blockIdx.x;
     if (!order.tile(block, tm, tn)) return;
-    const uint32_t from = (wave * 8 + lane / 8) * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+    const uint32_t from = (wave * 8 + lane / 8) * pitch + ((lane % 8) ^ (wave % 2 * 4 + lane / 16)) * 16;
     WideLoads loads;
     loads.set(A, B, tm, tn, pitch, spitch, wave, lane);
-    uint32_t sa[4], sb[4], next_sa[4], next_sb[4];
+    uint32_t scales[8], words[4];   // of this stage (a's fragments, then b's), as loaded for the next
+    // the words of 64 rows: those of 32 rows in both halves of the wave
+    auto spread = [](uint32_t word, uint32_t& low, uint32_t& high) {
+        const auto w = __builtin_amdgcn_permlane32_swap(word, word, false, false);
+        low = w[0];
+        high = w[1];
+    };
     struct Fragments {
         Codes32 a[4], b[4];
     } even, odd;   // columns [0, 64) and [64, 128) of a stage
     // a lane reads chunks 4 h + lane / 32 and the second behind it of row lane % 32
-    const uint32_t at = lane % 32 * 128 + ((lane / 32) ^ (lane % 8)) * 16;
-    auto read = [&](Fragments& f, uint32_t stage, int h) {
-        const uint8_t* x = lds + stage + (at ^ (h * 64));
-        const uint8_t* y = lds + stage + (at ^ (h * 64 + 32));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f.b[i].half[0] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
-            f.b[i].half[1] = *reinterpret_cast<const u32x4*>(y + (kWideTile + wn + i * 32) * 128);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f.a[i].half[0] = *reinterpret_cast<const u32x4*>(x + (wm + i * 32) * 128);
-            f.a[i].half[1] = *reinterpret_cast<const u32x4*>(y + (wm + i * 32) * 128);
-        }
+    const uint32_t at = lane % 32 * 128 + ((lane / 32) ^ (lane / 2 % 8)) * 16;
+    // the q-th of a half stage's 16 reads
+    auto read = [&](Fragments& f, uint32_t stage, int h, auto q) {
+        constexpr int i = q / 2 % 4, part = q % 2;
+        const uint8_t* x = lds + stage + (at ^ (h * 64 + part * 32));
+        if constexpr (q < 8) f.b[i].half[part] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
+        else f.a[i].half[part] = *reinterpret_cast<const u32x4*>(x + (wm + i * 32) * 128);
     };
-    loads.fetch_scales(sa, sb);
-    loads.fetch(lds, from, pitch, wave);
+    loads.fetch_all(lds, from, pitch, wave, words);
     loads_done();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) spread(words[i], scales[2 * i], scales[2 * i + 1]);
     loads.stage = 1;
-    loads.fetch_scales(next_sa, next_sb);
-    loads.fetch(lds + kStage, from, pitch, wave);
-    read(even, 0, 0);
+    loads.fetch_all(lds + kStage, from, pitch, wave, words);
+    unrolled<16>([&](auto q) { read(even, 0, 0, q); });
     uint32_t here = 0;
+    bool four = false;   // whether `words` holds four stages' scales, and not nothing
     for (;;) {
         f32x16 acc[4][4];
 #pragma unroll
@@ -217,13 +224,10 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-        auto multiply = [&](const Fragments& f) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j].all, f.a[i].all, acc[i][j], 0, 0, 0,
-                                                                               sb[j], 0, sa[i]);
+        auto multiply = [&](const Fragments& f, auto q) {
+            constexpr int i = q / 4, j = q % 4;
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j].all, f.a[i].all, acc[i][j], 0, 0, 0,
+                                                                       scales[4 + j], 0, scales[i]);
         };
         block += gridDim.x;
         const bool more = order.tile(block, next_tm, next_tn);
@@ -237,18 +241,35 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             }
 #pragma unroll 1
             for (uint32_t t = last_two ? stages - 2 : 0; t < (last_two ? stages : stages - 2); ++t) {
-                read(odd, here, 1);
-                multiply(even);
-                interleave_reads<16>();
+                // The order is the source's: a product, a read and a load at a time. (The
+                // compiler put the loads in one burst, and moves of scales behind it, which
+                // waited for them: 243 us instead of 230. Two loads at a time 231, as they
+                // take 16 cycles of the compute unit's 64 a product.)
+                unrolled<16>([&](auto q) {
+                    multiply(even, q);
+                    read(odd, here, 1, q);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
                 loads_done();   // this stage is in every wave's registers, and the next has arrived
-                read(even, here ^ kStage, 0);
-                multiply(odd);
+                uint32_t then[8];   // the next stage's scales
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sa[i] = next_sa[i], sb[i] = next_sb[i];
+                for (int i = 0; i < 4; ++i) {
+                    spread(words[i], then[2 * i], then[2 * i + 1]);
+                    then[2 * i] = four ? then[2 * i] : scales[2 * i] >> 8;
+                    then[2 * i + 1] = four ? then[2 * i + 1] : scales[2 * i + 1] >> 8;
+                    asm volatile("" : "+v"(then[2 * i]), "+v"(then[2 * i + 1]));   // done here, not behind the loads
+                }
                 ++loads.stage;
-                loads.fetch_scales(next_sa, next_sb);
-                loads.fetch(lds + here, from, pitch, wave);
-                interleave_reads<16>();
+                four = loads.first_of_four();
+                unrolled<16>([&](auto q) {
+                    multiply(odd, q);
+                    read(even, here ^ kStage, 0, q);
+                    loads.fetch(q, lds + here, from, pitch, wave);
+                    if constexpr (q < 4) loads.fetch_scales(q, words);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+#pragma unroll
+                for (int i = 0; i < 8; ++i) scales[i] = then[i];
                 here ^= kStage;
             }
         }
@@ -314,7 +335,7 @@ __global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Opera
     for (int i = 0; i < kLoads; ++i) {
         const bool a = i < TM * 2;
         const int64_t r = a ? min(m0 + i * 8 + lane / 8, A.rows - 1) : min(n0 + (i - TM * 2) * 8 + lane / 8, B.rows - 1);
-        from[i] = (a ? A.codes : B.codes) + r * pitch + ((lane % 8) ^ (lane / 8)) * 16;
+        from[i] = (a ? A.codes : B.codes) + r * pitch + ((lane % 8) ^ (i % 2 * 4 + lane / 16)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) sa[i] = A.scales + (min(m0 + i * 16 + lane % 16, A.rows - 1) >> A.shift) * spitch;
@@ -340,7 +361,7 @@ __global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Opera
             for (int i = 0; i < kLoads; ++i) load_lds16(from[i] + s * 128, ring + d * kSlot + i * 1024);
         };
         unrolled<D>([&](auto d) { fetch(begin + decltype(d)::value, decltype(d)::value); });
-        const int at = lane % 16 * 128 + ((lane / 16) ^ (lane % 8)) * 16;
+        const int at = lane % 16 * 128 + ((lane / 16) ^ (lane / 2 % 8)) * 16;
         for (uint32_t base = begin; base < end; base += D)
             unrolled<D>([&](auto dc) {
                 constexpr int d = decltype(dc)::value;
@@ -443,14 +464,14 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     if (fits(64, 32)) return launch_narrow<4, 2, 8, 1, Exact, OT>(a, b, k, out, s);
     if (fits(64, 64)) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
     if constexpr (!Exact) {
-        // A round of 256 x 256 tiles takes about 1.5 times one of two 128 x 128 tiles
-        // per compute unit, which hold half of it: k = 4096, us, wide / 128 x 128:
-        // 2048x4096 55 / 39, 2560x4096 56 / 60, 4608x4096 106 / 93, 6144x4096 108 / 109,
-        // 8192x8192 228 / 286.
+        // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
+        // compute unit, which hold half of it: k = 4096, us, wide / 128 x 128: 2048x4096
+        // 43 / 41, 2304x4096 44 / 61, 4096x4096 57 / 78, 4608x4096 93 / 97, 6144x4096
+        // 97 / 116, 8192x8192 217 / 302.
         const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
         const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
         if (a.rows >= kWideTile && b.rows >= kWideTile && b.rows <= (1 << 24) && k > 128 &&
-            3 * ceil_div(wide.tiles(), 256) < 2 * ceil_div(tiles, 512)) {
+            ceil_div(wide.tiles(), 256) < ceil_div(tiles, 512)) {
             hipLaunchKernelGGL(matmul8_wide_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8))), dim3(256), 0, s, a, b,
                                static_cast<uint32_t>(pitch8(k)), static_cast<uint32_t>(scale_pitch8(k)), wide,
                                static_cast<OT*>(out));

@@ -60,6 +60,9 @@ struct Buffer {
     __device__ __forceinline__ u32x4 load16(uint32_t offset) const {
         return __builtin_amdgcn_raw_buffer_load_b128(rsrc, offset, 0, 0);
     }
+    __device__ __forceinline__ uint32_t load4(uint32_t offset, uint32_t uniform) const {
+        return __builtin_amdgcn_raw_buffer_load_b32(rsrc, offset, uniform, 0);
+    }
     __device__ __forceinline__ uint32_t load1(uint32_t offset) const {
         return __builtin_amdgcn_raw_buffer_load_b8(rsrc, offset, 0, 0);
     }
