@@ -239,32 +239,23 @@ __global__ __launch_bounds__(256) void weight_grad8_wide_kernel(const uint16_t* 
         u32x4 g[8], c[4];
         uint32_t s[4];
     } one, two;   // even and odd stages
-    auto fetch = [&](Staged& to, int stage) {
-        const Rows rows(grad, x, scales, begin + stage * static_cast<int64_t>(kStep), end, m, n, n0, pitch, spitch, k0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to.s[i] = rows.scales.load1(scale_at[i]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to.c[i] = rows.x.load16(x_at[i]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) to.g[i] = rows.grad.load16(grad_at[i]);
+    Rows rows(grad, x, scales, begin, end, m, n, n0, pitch, spitch, k0);   // of the stage that is loaded next
+    // the q-th of a stage's 16 loads
+    auto fetch = [&](Staged& to, auto q) {
+        if constexpr (q < 4) to.s[q] = rows.scales.load1(scale_at[q]);
+        else if constexpr (q < 8) to.c[q - 4] = rows.x.load16(x_at[q - 4]);
+        else to.g[q - 8] = rows.grad.load16(grad_at[q - 8]);
     };
-    auto keep = [&](const Staged& from, int stage) {
+    // an eighth of a stage's way into LDS: 8 columns of x of one of a lane's rows, and of grad
+    auto keep = [&](const Staged& from, int stage, auto q) {
         uint8_t* to = lds + (stage & 1) * kStage;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 16 + t / 16;
-            const float f = scale_value(from.s[i]);
-            const u32x4& c = from.c[i];
-            const u32x2 a = widen4(c[0], f), b = widen4(c[1], f), d = widen4(c[2], f), e = widen4(c[3], f);
-            u32x4* p = reinterpret_cast<u32x4*>(to + kOperand + row * kRow + ((t % 16) ^ (row % 4 * 2)) * 32);
-            p[0] = u32x4{a[0], a[1], b[0], b[1]};
-            p[1] = u32x4{d[0], d[1], e[0], e[1]};
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = i * 8 + t / 32;
-            *reinterpret_cast<u32x4*>(to + row * kRow + ((t % 32 / 2) ^ (row % 4 * 2)) * 32 + t % 2 * 16) = from.g[i];
-        }
+        constexpr int i = q / 2, part = q % 2;
+        const int row = i * 16 + t / 16, g_row = q * 8 + t / 32;
+        const float f = scale_value(from.s[i]);
+        const u32x2 a = widen4(from.c[i][2 * part], f), b = widen4(from.c[i][2 * part + 1], f);
+        *reinterpret_cast<u32x4*>(to + kOperand + row * kRow + ((t % 16) ^ (row % 4 * 2)) * 32 + part * 16) =
+            u32x4{a[0], a[1], b[0], b[1]};
+        *reinterpret_cast<u32x4*>(to + g_row * kRow + ((t % 32 / 2) ^ (g_row % 4 * 2)) * 32 + t % 2 * 16) = from.g[q];
     };
 
     struct Fragments {
@@ -277,12 +268,11 @@ __global__ __launch_bounds__(256) void weight_grad8_wide_kernel(const uint16_t* 
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         piece[j] = row_of * kRow + ((j * 2 + lane / 16 % 2) ^ (lane % 16 / 4 * 2)) * 32 + lane % 4 * 8;
-    auto read = [&](Fragments& f, int stage, int chunk) {
+    // the q-th of 8 fragments of a stage's 16 rows number `chunk`
+    auto read = [&](Fragments& f, int stage, int chunk, auto q) {
         const uint8_t* at = lds + (stage & 1) * kStage + chunk * 16 * kRow;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f.x[j] = read_transposed(at + kOperand + wk * 2 + piece[j], 4 * kRow);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f.g[j] = read_transposed(at + wn * 2 + piece[j], 4 * kRow);
+        if constexpr (q < 4) f.x[q] = read_transposed(at + kOperand + wk * 2 + piece[q], 4 * kRow);
+        else f.g[q - 4] = read_transposed(at + wn * 2 + piece[q - 4], 4 * kRow);
     };
     f32x16 acc[4][4];
 #pragma unroll
@@ -291,40 +281,47 @@ __global__ __launch_bounds__(256) void weight_grad8_wide_kernel(const uint16_t* 
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-    auto multiply = [&](const Fragments& f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[j], f.g[i], acc[i][j], 0, 0, 0);
+    auto multiply = [&](const Fragments& f, auto q) {
+        constexpr int i = q / 4, j = q % 4;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.x[j], f.g[i], acc[i][j], 0, 0, 0);
     };
-    fetch(one, 0);
-    fetch(two, 1);
-    keep(one, 0);
+    auto next_rows = [&](int stage) {
+        rows = Rows(grad, x, scales, begin + stage * static_cast<int64_t>(kStep), end, m, n, n0, pitch, spitch, k0);
+    };
+    unrolled<16>([&](auto q) { fetch(one, q); });
+    next_rows(1);
+    unrolled<16>([&](auto q) { fetch(two, q); });
+    unrolled<8>([&](auto q) { keep(one, 0, q); });
     __syncthreads();
-    keep(two, 1);
-    read(even, 0, 0);
+    unrolled<8>([&](auto q) { keep(two, 1, q); });
+    unrolled<8>([&](auto q) { read(even, 0, 0, q); });
     __builtin_amdgcn_sched_barrier(0);
-    fetch(one, 2);
+    next_rows(2);
+    unrolled<16>([&](auto q) { fetch(one, q); });
+    next_rows(3);
+    // The order is the source's, a load behind every third product (left to the compiler,
+    // two behind each of the first eight: 496 us instead of 448, as the loads' addresses
+    // take the compute unit as long as a product).
     auto run = [&](const Staged& mine, Staged& other, int stage) {
-        read(odd, stage, 1);
-        fetch(other, stage + 3);
-        multiply(even);
-        interleave_reads<16>();
-        __builtin_amdgcn_sched_barrier(0);
-        read(even, stage, 2);
-        multiply(odd);
-        interleave_reads<16>();
-        __builtin_amdgcn_sched_barrier(0);
-        read(odd, stage, 3);
-        multiply(even);
-        interleave_reads<16>();
+        unrolled<3>([&](auto c) {
+            const Fragments& now = c % 2 ? odd : even;
+            Fragments& then = c % 2 ? even : odd;
+            unrolled<16>([&](auto q) {
+                multiply(now, q);
+                if constexpr (q % 2 == 0) read(then, stage, c + 1, std::integral_constant<int, q / 2>{});
+                constexpr int at = c * 16 + q;
+                if constexpr (at % 3 == 1) fetch(other, std::integral_constant<int, at / 3>{});
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
         lds_done();
-        keep(mine, stage + 2);
-        read(even, stage + 1, 0);
-        multiply(odd);
-        interleave_writes();
-        __builtin_amdgcn_sched_barrier(0);
+        unrolled<16>([&](auto q) {
+            multiply(odd, q);
+            if constexpr (q < 8) keep(mine, stage + 2, q);
+            else read(even, stage + 1, 0, std::integral_constant<int, q - 8>{});
+            if constexpr (q == 12) next_rows(stage + 4);
+            __builtin_amdgcn_sched_barrier(0);
+        });
     };
     // (a stage behind the last one holds zeros)
 #pragma unroll 1
@@ -401,26 +398,32 @@ struct Way {
 };
 
 // The way with the least estimated time. A stage of 64 rows takes 1.7 us of a compute
-// unit with 256 x 256 outputs (one workgroup), 1.2 with 128 x 128 (each of two) and with
-// 64 x 64 (each of four); a workgroup's start and end 8, 4 and 3 us; parts are
-// written and read again at 1.5 bytes a ns. Measured, us, with tiles of 256 / 128 / 64
-// only (m x n x k): 16384x4096x4096 456 / 592 / 946, 8192x2048x2048 85 / 88 / 128,
-// 2048x4096x1024 47 / 35 / 38, 1024x1024x1024 31 / 19 / 10, 4099x300x515 33 / 19 / 16. At 5
-// bytes a ns the parts were too many: 1024x1024x1024 15, 16384x256x256 26 instead of 22.
+// unit with 256 x 256 outputs (one workgroup), 0.84 or 1.2 with 128 x 128 (one or two), and
+// 0.45 to 1.2 with 64 x 64 (one to four); a workgroup's start and end 8, 4 and 3 us; parts
+// are written and read again at 5 bytes a ns, and each takes 0.1 us. Measured, us, with
+// tiles of 256 / 128 / 64 only (m x n x k): 16384x4096x4096 438 / 604 / 970, 4096x4096x4096
+// 120 / 160 / 254, 3000x5000x2000 78 / 92 / 128, 8192x2048x2048 88 / 91 / 130,
+// 2048x4096x1024 56 / 31 / 39, 1024x1024x1024 33 / 18 / 10, 4099x300x515 26 / 15 / 13. With
+// parts at 1.5 bytes a ns they were too few (6000x1000x1000 41 instead of 30).
 Way way_of(int64_t m, int64_t n, int64_t k) {
     Way best{128, 1, 0};
     double least = 0;
     const int64_t stages = ceil_div(m, kStep);
     for (int tile = 256; tile >= 64; tile /= 2) {
         if (tile == 256 && (n < 256 || pitch8(k) < 256)) continue;
-        const int64_t tiles = ceil_div(n, tile) * ceil_div(k, tile), at_once = device_cus() * (tile == 256 ? 1 : tile == 128 ? 2 : 4);
-        const double stage_us = tile == 256 ? 1.7 : 1.2, fixed_us = tile == 256 ? 8 : tile == 128 ? 4 : 3;
+        const int64_t tiles = ceil_div(n, tile) * ceil_div(k, tile), cus = device_cus(), most_of_cu = tile == 256 ? 1 : tile == 128 ? 2 : 4;
+        const double fixed_us = tile == 256 ? 8 : tile == 128 ? 4 : 3;
+        const auto stage_us = [&](int64_t of_cu) {   // with so many workgroups on a compute unit
+            return tile == 256 ? 1.7 : tile == 128 ? 0.48 + 0.36 * of_cu : 0.2 + 0.25 * of_cu;
+        };
         const int64_t most = n * k > kMaxSplit ? 1 : std::min<int64_t>(stages, 64);
         for (int64_t count = 1; count <= most; ++count) {
             const int64_t each = ceil_div(stages, count);
             if (count > 1 && ceil_div(stages, each) != count) continue;
-            const double us = ceil_div(tiles * count, at_once) * (each * stage_us + fixed_us) +
-                              (count > 1 ? 3 + count * 8.0 * n * k / 1.5e6 : 0);
+            const int64_t rounds = tiles * count / (cus * most_of_cu), rest = tiles * count - rounds * cus * most_of_cu;
+            const double us = rounds * (each * stage_us(most_of_cu) + fixed_us) +
+                              (rest > 0 ? each * stage_us(ceil_div(rest, cus)) + fixed_us : 0) +
+                              (count > 1 ? 3 + count * (0.1 + n * k / 0.6e6) : 0);
             if (least == 0 || us < least) least = us, best = Way{tile, static_cast<int>(count), each * kStep};
         }
     }
