@@ -462,7 +462,11 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     if (fits(32, 16)) return launch_narrow<2, 1, 8, 2, Exact, OT>(a, b, k, out, s);
     if (fits(32, 32)) return launch_narrow<2, 2, 8, 2, Exact, OT>(a, b, k, out, s);
     if (fits(64, 32)) return launch_narrow<4, 2, 8, 1, Exact, OT>(a, b, k, out, s);
-    if (fits(64, 64)) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
+    // On bfloat16 a stage of 128 x 128 outputs takes twice as long, and two rounds of
+    // 64 x 64 are faster where there are many: us, 64 x 64 / 128 x 128: 1792x848x2804 23 / 28,
+    // 166x6658x2723 22 / 28, 1402x951x1610 18 / 18, 794x1835x724 13 / 11.
+    const bool two_rounds = Exact && k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * device_cus();
+    if (fits(64, 64) || two_rounds) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
     if constexpr (!Exact) {
         // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
         // compute unit, which hold half of it: k = 4096, us, wide / 128 x 128: 2048x4096

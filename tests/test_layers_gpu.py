@@ -395,7 +395,7 @@ def check_product(m, n, k, ablock, bblock, odt, seed=0, spread=2.0):
     (1, 1, 1), (1, 16, 128), (2, 17, 129), (16, 128, 512), (17, 130, 640), (33, 1000, 777), (64, 64, 4096),
     (65, 48, 300), (127, 129, 1024), (128, 128, 128), (129, 257, 257), (200, 520, 1537), (256, 256, 256),
     (300, 1025, 520), (513, 700, 640), (1100, 2050, 384), (2100, 4001, 300), (2304, 4100, 1152), (4097, 2090, 200), (2050, 4097, 90),
-    (500, 510, 200), (1000, 1023, 400), (1024, 1000, 130), (6200, 8200, 300)])
+    (500, 510, 200), (1791, 849, 2100), (1000, 1023, 400), (1024, 1000, 130), (6200, 8200, 300)])
 def test_matmul8(odt, m, n, k):
     check_product(m, n, k, 1, 128, odt, seed=m + n + k)
 
