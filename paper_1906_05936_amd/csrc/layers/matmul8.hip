@@ -124,7 +124,9 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 // stages ahead, across the end of a tile: the next one's first stages arrive
 // while this one's outputs leave. 8192 x 8192 x 4096: 209 to 217 us, 2.5 to 2.6
 // PFLOP/s; the matrix units are busy for two thirds of the cycles, at a clock that
-// the power they take brings down to 1.9 GHz.
+// the power they take brings down to 1.9 GHz. Exact: a wave widens the fragments by
+// quarters (for instructions of 32 x 32 x 16), one while the one before it is
+// multiplied: 386 us, 1.42 PFLOP/s (128 x 128 outputs 495).
 constexpr int kWideTile = 256;
 
 // The stage that a workgroup loads next: tile, place in it, addresses. The last
@@ -176,8 +178,9 @@ struct WideLoads {
     }
 };
 
+template <bool Exact, typename OT>
 __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
-                                                           TileOrder order, uint16_t* __restrict__ out) {
+                                                           TileOrder order, OT* __restrict__ out) {
     constexpr int kStage = WideLoads::kStage;
     __shared__ __align__(16) uint8_t lds[2 * kStage + 4 * 8192];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -202,9 +205,9 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
     const uint32_t at = lane % 32 * 128 + ((lane / 32) ^ (lane / 2 % 8)) * 16;
     // the q-th of a half stage's 16 reads
     auto read = [&](Fragments& f, uint32_t stage, int h, auto q) {
-        constexpr int i = q / 2 % 4, part = q % 2;
+        constexpr int i = Exact ? q % 4 : q / 2 % 4, part = Exact ? q / 8 : q % 2;
         const uint8_t* x = lds + stage + (at ^ (h * 64 + part * 32));
-        if constexpr (q < 8) f.b[i].half[part] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
+        if constexpr (Exact ? q % 8 < 4 : q < 8) f.b[i].half[part] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
         else f.a[i].half[part] = *reinterpret_cast<const u32x4*>(x + (wm + i * 32) * 128);
     };
     loads.fetch_all(lds, from, pitch, wave, words);
@@ -214,6 +217,18 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
     loads.stage = 1;
     loads.fetch_all(lds + kStage, from, pitch, wave, words);
     unrolled<16>([&](auto q) { read(even, 0, 0, q); });
+    // Exact: a quarter of a half stage in bfloat16 (a lane's 8 columns of every row), and
+    // the next one, whose e-th of 32 steps this is
+    struct Widened {
+        uint32_t a[4][4], b[4][4];
+    } quarter[2];
+    auto widen = [&](const Fragments& f, const uint32_t (&s)[8], auto g, auto e) {
+        constexpr int i = e / 8, word = g * 2 + e % 4 / 2;
+        const float sa = scale_value(s[i] & 0xffu), sb = scale_value(s[4 + i] & 0xffu);
+        if constexpr (e % 8 < 4) quarter[g % 2].a[i][e % 4] = widen2<e % 2>(f.a[i].word[word], sa);
+        else quarter[g % 2].b[i][e % 4] = widen2<e % 2>(f.b[i].word[word], sb);
+    };
+    if constexpr (Exact) unrolled<32>([&](auto e) { widen(even, scales, std::integral_constant<int, 0>{}, e); });
     uint32_t here = 0;
     bool four = false;   // whether `words` holds four stages' scales, and not nothing
     for (;;) {
@@ -228,6 +243,28 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             constexpr int i = q / 4, j = q % 4;
             acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j].all, f.a[i].all, acc[i][j], 0, 0, 0,
                                                                        scales[4 + j], 0, scales[i]);
+        };
+        // Exact: a half stage, 64 products of 32 x 32 x 16. Meanwhile the next half is read
+        // and, by quarters, widened (`then`: its scales).
+        auto half = [&](const Fragments& f, Fragments& next, uint32_t stage, int h, const uint32_t (&then)[8], auto fetch) {
+            unrolled<4>([&](auto g) {
+                unrolled<16>([&](auto q) {
+                    constexpr int i = q / 4, j = q % 4, at = g * 16 + q;
+                    const auto eight = [](const uint32_t (&x)[4]) {
+                        return __builtin_bit_cast(bf16x8, u32x4{x[0], x[1], x[2], x[3]});
+                    };
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(quarter[g % 2].b[j]), eight(quarter[g % 2].a[i]),
+                                                                        acc[i][j], 0, 0, 0);
+                    unrolled<2>([&](auto u) {
+                        using E = std::integral_constant<int, q * 2 + u>;
+                        if constexpr (g < 3) widen(f, scales, std::integral_constant<int, g + 1>{}, E{});
+                        else widen(next, then, std::integral_constant<int, 0>{}, E{});
+                    });
+                    if constexpr (at % 4 == 0) read(next, stage, h, std::integral_constant<int, at / 4>{});
+                    if constexpr (at % 4 == 2) fetch(std::integral_constant<int, at / 4>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
         };
         block += gridDim.x;
         const bool more = order.tile(block, next_tm, next_tn);
@@ -245,7 +282,9 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
                 // compiler put the loads in one burst, and moves of scales behind it, which
                 // waited for them: 243 us instead of 230. Two loads at a time 231, as they
                 // take 16 cycles of the compute unit's 64 a product.)
-                unrolled<16>([&](auto q) {
+                if constexpr (Exact)
+                    half(even, odd, here, 1, scales, [](auto) {});
+                else unrolled<16>([&](auto q) {
                     multiply(even, q);
                     read(odd, here, 1, q);
                     __builtin_amdgcn_sched_barrier(0);
@@ -261,7 +300,12 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
                 }
                 ++loads.stage;
                 four = loads.first_of_four();
-                unrolled<16>([&](auto q) {
+                if constexpr (Exact)
+                    half(odd, even, here ^ kStage, 0, then, [&](auto q) {
+                        loads.fetch(q, lds + here, from, pitch, wave);
+                        if constexpr (q < 4) loads.fetch_scales(q, words);
+                    });
+                else unrolled<16>([&](auto q) {
                     multiply(odd, q);
                     read(even, here ^ kStage, 0, q);
                     loads.fetch(q, lds + here, from, pitch, wave);
@@ -273,35 +317,47 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
                 here ^= kStage;
             }
         }
-        // 32 rows of the wave's outputs at a time pass through LDS (16-byte chunks
-        // exchanged by row), so that rows leave in runs of 256 bytes
+        // 32 rows of the wave's outputs, 256 bytes of each, at a time pass through LDS
+        // (16-byte chunks exchanged by row), so that rows leave in runs
         uint32_t l = lane;
         asm volatile("" : "+v"(l));   // the addresses below are not worth registers during the products
+        constexpr int kPart = 256 / (32 * sizeof(OT));   // fragments of 32 columns in 256 bytes
+        const uint64_t row_bytes = static_cast<uint64_t>(B.rows) * sizeof(OT);
         uint8_t* o = reinterpret_cast<uint8_t*>(out + (WideLoads::origin(tm, A.rows) + wm) * B.rows +
-                                                WideLoads::origin(tn, B.rows) + wn);
-        const uint32_t row_bytes = static_cast<uint32_t>(B.rows) * 2, lane_at = l / 16 * row_bytes + l % 16 * 16;
+                                                WideLoads::origin(tn, B.rows) + wn) + l / 16 * row_bytes + l % 16 * 16;
         uint8_t* mine = lds + 2 * kStage + wave * 8192;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                asm volatile("" : "+a"(acc[i][j]));   // read from its accumulation registers here, not earlier
+            for (int p = 0; p < 4 / kPart; ++p) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    *reinterpret_cast<u32x2*>(mine + l % 32 * 256 + ((j * 4 + r) ^ (l % 16)) * 16 + l / 32 * 8) =
-                        u32x2{f32_to_bf16x2(acc[i][j][r * 4], acc[i][j][r * 4 + 1]),
-                              f32_to_bf16x2(acc[i][j][r * 4 + 2], acc[i][j][r * 4 + 3])};
+                for (int u = 0; u < kPart; ++u) {
+                    f32x16& v = acc[i][p * kPart + u];
+                    asm volatile("" : "+a"(v));   // read from its accumulation registers here, not earlier
+                    uint8_t* row = mine + l % 32 * 256;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (Exact)
+                            *reinterpret_cast<f32x4*>(row + ((u * 8 + r * 2 + l / 32) ^ (l % 16)) * 16) =
+                                f32x4{v[r * 4], v[r * 4 + 1], v[r * 4 + 2], v[r * 4 + 3]};
+                        else
+                            *reinterpret_cast<u32x2*>(row + ((u * 4 + r) ^ (l % 16)) * 16 + l / 32 * 8) =
+                                u32x2{f32_to_bf16x2(v[r * 4], v[r * 4 + 1]), f32_to_bf16x2(v[r * 4 + 2], v[r * 4 + 3])};
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                __builtin_amdgcn_wave_barrier();
+                uint8_t* to = o + p * 256;
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    const uint32_t row = q * 4 + l / 16;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 256 + ((l % 16) ^ (row % 16)) * 16);
+                    __builtin_nontemporal_store(u32x4_u2{v[0], v[1], v[2], v[3]}, reinterpret_cast<u32x4_u2*>(to));
+                    to += 4 * row_bytes;
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const uint32_t row = q * 4 + l / 16;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * 256 + ((l % 16) ^ (row % 16)) * 16);
-                __builtin_nontemporal_store(u32x4_u2{v[0], v[1], v[2], v[3]}, reinterpret_cast<u32x4_u2*>(o + lane_at));
-                o += 4 * static_cast<uint64_t>(row_bytes);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            o += 32 * row_bytes;
         }
         if (!more) break;
         tm = next_tm;
@@ -467,20 +523,18 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     // 166x6658x2723 22 / 28, 1402x951x1610 18 / 18, 794x1835x724 13 / 11.
     const bool two_rounds = Exact && k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * device_cus();
     if (fits(64, 64) || two_rounds) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
-    if constexpr (!Exact) {
-        // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
-        // compute unit, which hold half of it: k = 4096, us, wide / 128 x 128: 2048x4096
-        // 43 / 41, 2304x4096 44 / 61, 4096x4096 57 / 78, 4608x4096 93 / 97, 6144x4096
-        // 97 / 116, 8192x8192 217 / 302.
-        const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
-        const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
-        if (a.rows >= kWideTile && b.rows >= kWideTile && b.rows <= (1 << 24) && k > 128 &&
-            ceil_div(wide.tiles(), 256) < ceil_div(tiles, 512)) {
-            hipLaunchKernelGGL(matmul8_wide_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8))), dim3(256), 0, s, a, b,
-                               static_cast<uint32_t>(pitch8(k)), static_cast<uint32_t>(scale_pitch8(k)), wide,
-                               static_cast<OT*>(out));
-            return check_launch("lsgd_matmul8");
-        }
+    // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
+    // compute unit, which hold half of it: k = 4096, us, wide / 128 x 128: 2048x4096
+    // 43 / 41, 2304x4096 44 / 61, 4096x4096 57 / 78, 4608x4096 93 / 97, 6144x4096
+    // 97 / 116, 8192x8192 217 / 302; Exact 70 / 65, 73 / 94, 104 / 127, 163 / 152,
+    // 172 / 192, 386 / 495.
+    const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
+    const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
+    if (a.rows >= kWideTile && b.rows >= kWideTile && k > 128 && ceil_div(wide.tiles(), 256) < ceil_div(tiles, 512)) {
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8)));
+        hipLaunchKernelGGL((matmul8_wide_kernel<Exact, OT>), grid, dim3(256), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
+                           static_cast<uint32_t>(scale_pitch8(k)), wide, static_cast<OT*>(out));
+        return check_launch("lsgd_matmul8");
     }
     return launch_tiles<4, 4, 2, 2, Exact, OT>(a, b, k, out, s);
 }

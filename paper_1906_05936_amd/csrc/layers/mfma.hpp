@@ -122,12 +122,15 @@ union Codes32 {
     uint32_t word[8];
 };
 
-// The 4 codes of a word times 2^(byte - 127), as bfloat16: exact unless below
-// 2^-126 or beyond its range.
+// The lower or upper 2 codes of a word times 2^(byte - 127), as bfloat16: exact unless
+// below 2^-126 or beyond its range; and all 4.
+template <int Upper>
+__device__ __forceinline__ uint32_t widen2(uint32_t codes, float scale) {
+    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, Upper != 0);
+    return __builtin_bit_cast(uint32_t, v);
+}
 __device__ __forceinline__ u32x2 widen4(uint32_t codes, float scale) {
-    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false);
-    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
-    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+    return u32x2{widen2<0>(codes, scale), widen2<1>(codes, scale)};
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
