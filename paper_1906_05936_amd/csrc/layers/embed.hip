@@ -452,15 +452,18 @@ __device__ __forceinline__ uint32_t pieces_behind(const uint32_t* key, uint32_t 
 
 // Rows of several pieces: a workgroup adds the slot 2c + 1 of the piece c in which
 // the row starts and the following pieces' slots 2c, divided over its waves in
-// order, then the waves' sums in order. It looks at kJoin pieces, 512 columns.
-constexpr uint32_t kJoin = 8;
-constexpr int kJoinThreads = 512;
+// order, then the waves' sums in order. It looks at a few pieces, 512 columns. A
+// frequent row takes as long as a wave has slots to add, so with small pieces twice the
+// waves look at half the pieces (118000 entries of 40, a tenth in one row: 88 us
+// instead of 102; with large ones, 131072 of 2048, 370 instead of 362).
+constexpr uint32_t join_pieces(int piece) { return piece == kFewPiece ? 4 : 8; }
+constexpr int join_threads(int piece) { return piece == kFewPiece ? 1024 : 512; }
 
 template <int kPiece, typename OT>
-__global__ __launch_bounds__(kJoinThreads) void join_pieces_kernel(Sorted s, uint32_t pieces, int64_t dim, uint32_t slabs,
+__global__ __launch_bounds__(join_threads(kPiece)) void join_pieces_kernel(Sorted s, uint32_t pieces, int64_t dim, uint32_t slabs,
                                                              float scale, const float* __restrict__ slots,
                                                              OT* __restrict__ out, bool accumulate) {
-    constexpr uint32_t kWaves = kJoinThreads / 64;
+    constexpr uint32_t kWaves = join_threads(kPiece) / 64, kJoin = join_pieces(kPiece);
     __shared__ float sums[kWaves - 1][512];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t c0 = blockIdx.x / slabs * kJoin;
@@ -736,8 +739,8 @@ lsgd_status sum_rows_of(const Workers& w, const Sorted& s, uint32_t n_tokens, ui
                        static_cast<uint32_t>(piece_blocks), slots, out, accumulate);
     LSGD_TRY(check_launch("lsgd_embed_grad"));
     if (pieces > 1) {
-        hipLaunchKernelGGL((join_pieces_kernel<kPiece, OT>), dim3(static_cast<unsigned>(ceil_div(pieces, kJoin) * slabs)),
-                           dim3(kJoinThreads), 0, st, s, static_cast<uint32_t>(pieces), dim, static_cast<uint32_t>(slabs), scale,
+        hipLaunchKernelGGL((join_pieces_kernel<kPiece, OT>), dim3(static_cast<unsigned>(ceil_div(pieces, join_pieces(kPiece)) * slabs)),
+                           dim3(join_threads(kPiece)), 0, st, s, static_cast<uint32_t>(pieces), dim, static_cast<uint32_t>(slabs), scale,
                            slots, out, accumulate);
         LSGD_TRY(check_launch("lsgd_embed_grad"));
     }

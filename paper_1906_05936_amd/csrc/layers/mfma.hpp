@@ -51,8 +51,9 @@ __device__ __forceinline__ void load_lds16(const void* global, void* lds) {
                                      0, 0);
 }
 
-// `bytes` from p on, addressed by a lane's 32-bit offset (plus a uniform one, which
-// the hardware's bounds check leaves out). Loads past the end give 0.
+// `bytes` from p on, addressed by a lane's 32-bit offset, plus a uniform one (both
+// together stay inside, whether or not the bounds check counts the uniform one).
+// Loads past the end give 0.
 struct Buffer {
     __amdgpu_buffer_rsrc_t rsrc;
     __device__ __forceinline__ Buffer(const void* p, uint32_t bytes)
