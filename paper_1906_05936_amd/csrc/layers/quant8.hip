@@ -64,12 +64,15 @@ __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict_
 }
 
 // Block 128. A workgroup holds a tile of 128 x 128 parameters in registers (a
-// lane: four times 4 rows by 4 columns), agrees on its largest magnitude, and
-// brings the codes into LDS as they are and transposed, from where every copy
-// is written in rows of 128 bytes. The transpose of each 4 x 4 happens in
-// registers. Bound by the parameters read and the copies written (8192 x 2048, four
-// copies and four transposed: 36 us, 5.6 TB/s; with stores through the caches 49);
-// up to kCopies copies a launch keep their pointers in the kernel's arguments.
+// lane: 4 rows by 4 columns), agrees on its largest magnitude, and brings the codes
+// into LDS as they are and transposed, from where every copy is written in rows
+// of 128 bytes. The transpose of each 4 x 4 happens in registers. Bound by the
+// parameters read and the copies written (8192 x 2048, four copies and four
+// transposed: 32 us, 6.3 TB/s; with stores through the caches 47), and where the
+// tiles are few by the way from load to store (1000 x 777: 4.9 us; with four 4 x 4 to
+// each of a quarter of the lanes 7.3, and 33 for the large one). Up to kCopies copies
+// a launch keep their pointers in the kernel's arguments.
+constexpr int kTileThreads = 1024;
 constexpr int kCopies = 32;
 constexpr int kRowWords = 33;    // LDS words per row of 128 codes: rows start in different banks
 
@@ -82,87 +85,61 @@ __device__ __forceinline__ void put_tile(const uint32_t (&tile)[128][kRowWords],
                                          int n, int64_t rows, int64_t cols, int64_t r0, int64_t c0) {
     const int64_t pitch = pitch8(cols), spitch = scale_pitch8(cols);
     const int64_t blocks = pitch / 128, cb = c0 / 128;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = i * 32 + threadIdx.x / 8, w = threadIdx.x % 8 * 4;
-        if (r0 + row < rows) {
-            const u32x4 v{tile[row][w], tile[row][w + 1], tile[row][w + 2], tile[row][w + 3]};
-            for (int k = 0; k < n; ++k)
-                __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to.codes[k] + (r0 + row) * pitch + c0 + w * 4));
-        }
+    const int row = threadIdx.x / 8, w = threadIdx.x % 8 * 4;
+    if (r0 + row < rows) {
+        const u32x4 v{tile[row][w], tile[row][w + 1], tile[row][w + 2], tile[row][w + 3]};
+        for (int k = 0; k < n; ++k)
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to.codes[k] + (r0 + row) * pitch + c0 + w * 4));
     }
     // the scale, and behind the last block of columns the row's padding
     const int64_t end = cb == blocks - 1 ? spitch : cb + 1;
-    for (int k = threadIdx.x; k < n; k += kBlock)
+    for (int k = threadIdx.x; k < n; k += kTileThreads)
         for (int64_t s = cb; s < end; ++s)
             to.scales[k][r0 / 128 * spitch + s] = static_cast<uint8_t>(s == cb ? byte : 127u);
 }
 
-__global__ __launch_bounds__(kBlock) void quant_blocks_kernel(const float* __restrict__ p, int64_t rows, int64_t cols,
-                                                              Copies plain, int n_plain, Copies transposed,
-                                                              int n_transposed) {
+__global__ __launch_bounds__(kTileThreads) void quant_blocks_kernel(const float* __restrict__ p, int64_t rows,
+                                                                    int64_t cols, Copies plain, int n_plain,
+                                                                    Copies transposed, int n_transposed) {
     __shared__ uint32_t tile[128][kRowWords];
-    __shared__ float wave_max[kBlock / 64];
+    __shared__ float wave_max[kTileThreads / 64];
     const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 128, r0 = static_cast<int64_t>(blockIdx.y) * 128;
     const int tr = threadIdx.x / 32 * 4, tc = threadIdx.x % 32 * 4;
     const int k = static_cast<int>(max(static_cast<int64_t>(0), min(cols - c0 - tc, static_cast<int64_t>(4))));
-    float v[4][4][4];
+    float v[4][4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int64_t r = r0 + a * 32 + tr + b;
-            const float* q = p + r * cols + c0 + tc;
-            const int kk = r < rows ? k : 0;
-            if (kk == 4) {
-                const f32x4_u x = *reinterpret_cast<const f32x4_u*>(q);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[a][b][i] = x[i];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[a][b][i] = i < kk ? q[i] : 0.0f;
-            }
-        }
+    for (int b = 0; b < 4; ++b) load4(p + (r0 + tr + b) * cols + c0 + tc, r0 + tr + b < rows ? k : 0, v[b]);
     float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 64; ++i) m = fmaxf(m, finite_abs((&v[0][0][0])[i]));
+    for (int i = 0; i < 16; ++i) m = fmaxf(m, finite_abs((&v[0][0])[i]));
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     if ((threadIdx.x & 63) == 0) wave_max[threadIdx.x >> 6] = m;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kBlock / 64; ++i) m = fmaxf(m, wave_max[i]);
+    for (int i = 0; i < kTileThreads / 64; ++i) m = fmaxf(m, wave_max[i]);
     const uint32_t byte = scale_byte(m);
     const float inv = inverse_scale(byte);
-    uint32_t q[4][4];
+    uint32_t q[4];
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-            q[a][b] = codes4(v[a][b][0] * inv, v[a][b][1] * inv, v[a][b][2] * inv, v[a][b][3] * inv);
+    for (int b = 0; b < 4; ++b) q[b] = codes4(v[b][0] * inv, v[b][1] * inv, v[b][2] * inv, v[b][3] * inv);
     if (n_plain > 0) {
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) tile[a * 32 + tr + b][tc / 4] = q[a][b];
+        for (int b = 0; b < 4; ++b) tile[tr + b][tc / 4] = q[b];
         __syncthreads();
         put_tile(tile, byte, plain, n_plain, rows, cols, r0, c0);
         __syncthreads();
     }
     if (n_transposed > 0) {
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            // bytes of (row b, column j) -> (column j, row b)
-            const uint32_t x0 = __builtin_amdgcn_perm(q[a][1], q[a][0], 0x05010400u);
-            const uint32_t x1 = __builtin_amdgcn_perm(q[a][1], q[a][0], 0x07030602u);
-            const uint32_t y0 = __builtin_amdgcn_perm(q[a][3], q[a][2], 0x05010400u);
-            const uint32_t y1 = __builtin_amdgcn_perm(q[a][3], q[a][2], 0x07030602u);
-            const int w = (a * 32 + tr) / 4;
-            tile[tc][w] = __builtin_amdgcn_perm(y0, x0, 0x05040100u);
-            tile[tc + 1][w] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);
-            tile[tc + 2][w] = __builtin_amdgcn_perm(y1, x1, 0x05040100u);
-            tile[tc + 3][w] = __builtin_amdgcn_perm(y1, x1, 0x07060302u);
-        }
+        // bytes of (row b, column j) -> (column j, row b)
+        const uint32_t x0 = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u);
+        const uint32_t x1 = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u);
+        const uint32_t y0 = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
+        const uint32_t y1 = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
+        tile[tc][tr / 4] = __builtin_amdgcn_perm(y0, x0, 0x05040100u);
+        tile[tc + 1][tr / 4] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);
+        tile[tc + 2][tr / 4] = __builtin_amdgcn_perm(y1, x1, 0x05040100u);
+        tile[tc + 3][tr / 4] = __builtin_amdgcn_perm(y1, x1, 0x07060302u);
         __syncthreads();
         put_tile(tile, byte, transposed, n_transposed, cols, rows, c0, r0);
     }
@@ -251,7 +228,7 @@ LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t c
             a.codes[i] = static_cast<uint8_t*>(codes[at + i]), a.scales[i] = static_cast<uint8_t*>(scales[at + i]);
         for (int i = 0; i < nb; ++i)
             b.codes[i] = static_cast<uint8_t*>(codes_t[at + i]), b.scales[i] = static_cast<uint8_t*>(scales_t[at + i]);
-        hipLaunchKernelGGL(quant_blocks_kernel, grid, dim3(kBlock), 0, static_cast<hipStream_t>(stream), params, rows,
+        hipLaunchKernelGGL(quant_blocks_kernel, grid, dim3(kTileThreads), 0, static_cast<hipStream_t>(stream), params, rows,
                            cols, a, na, b, nb);
         LSGD_TRY(check_launch("lsgd_copy_out8"));
     }
