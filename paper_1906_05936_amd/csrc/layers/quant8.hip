@@ -26,20 +26,33 @@ __device__ __forceinline__ float max_of_16(float a) {
 // scales leave as one word. Bound by the bytes of x read and codes written, as
 // long as it takes few instructions: fmaxf passes NaNs over, and only where an
 // infinity is left are the magnitudes looked at again. 16384 x 4096 bfloat16: 35 us,
-// 5.7 TB/s; with x kept in the caches, or a wave for every 512 columns, 39 to 42.
+// 5.8 TB/s; with x kept in the caches, or a wave for every 512 columns, 39 to 42.
+// binary32: 53 us, 6.4 TB/s, with 4 of a lane's columns in either half of the block, so
+// that an instruction reads whole lines, and neighbouring workgroups on the same
+// rows, a wave for every 512 columns; as for bfloat16 75 us, which with rows of
+// odd length is the other way round (8191: 38 us, along the rows 43 to 65).
 template <typename T>
 __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t cols,
                                                             int64_t pitch, int64_t spitch, uint32_t groups,
                                                             uint8_t* __restrict__ codes,
                                                             uint8_t* __restrict__ scales) {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int64_t r = static_cast<int64_t>(blockIdx.x) * (kBlock / 64) + wave; r < rows;
-         r += static_cast<int64_t>(gridDim.x) * (kBlock / 64)) {
-        for (uint32_t g = blockIdx.y; g < groups; g += gridDim.y) {
-            const int64_t c = static_cast<int64_t>(g) * 512 + lane * 8;
-            const int k = c < cols ? static_cast<int>(min(cols - c, static_cast<int64_t>(8))) : 0;
+    constexpr bool kHalves = sizeof(T) == 4;
+    const uint32_t at = kHalves ? blockIdx.y : blockIdx.x, of = kHalves ? gridDim.y : gridDim.x;
+    const uint32_t first = kHalves ? blockIdx.x : blockIdx.y, step = kHalves ? gridDim.x : gridDim.y;
+    for (int64_t r = static_cast<int64_t>(at) * (kBlock / 64) + wave; r < rows; r += static_cast<int64_t>(of) * (kBlock / 64)) {
+        for (uint32_t g = first; g < groups; g += step) {
+            const int64_t c = static_cast<int64_t>(g) * 512 + (kHalves ? lane / 16 * 128 + lane % 16 * 4 : lane * 8);
+            const auto inside = [&](int64_t from, int64_t most) {
+                return static_cast<int>(max(static_cast<int64_t>(0), min(cols - from, most)));
+            };
             float v[8];
-            load8_once(x + r * cols + c, k, v);
+            if constexpr (kHalves) {
+                load4_once(x + r * cols + c, inside(c, 4), v);
+                load4_once(x + r * cols + c + 64, inside(c + 64, 4), v + 4);
+            } else {
+                load8_once(x + r * cols + c, inside(c, 8), v);
+            }
             float a = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(v[i]));
@@ -52,9 +65,16 @@ __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict_
             const float inv = inverse_scale(byte);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= inv;
-            if (c < pitch)
-                *reinterpret_cast<u32x2*>(codes + r * pitch + c) =
-                    u32x2{codes4(v[0], v[1], v[2], v[3]), codes4(v[4], v[5], v[6], v[7])};
+            const uint32_t lo = codes4(v[0], v[1], v[2], v[3]), hi = codes4(v[4], v[5], v[6], v[7]);
+            if (c < pitch) {
+                uint8_t* q = codes + r * pitch + c;
+                if constexpr (kHalves) {
+                    *reinterpret_cast<uint32_t*>(q) = lo;
+                    *reinterpret_cast<uint32_t*>(q + 64) = hi;
+                } else {
+                    *reinterpret_cast<u32x2*>(q) = u32x2{lo, hi};
+                }
+            }
             const uint32_t word = __builtin_amdgcn_readlane(byte, 0) | __builtin_amdgcn_readlane(byte, 16) << 8 |
                                   __builtin_amdgcn_readlane(byte, 32) << 16 |
                                   static_cast<uint32_t>(__builtin_amdgcn_readlane(byte, 48)) << 24;
@@ -172,11 +192,14 @@ LSGD_API lsgd_status lsgd_quant8(const void* x, lsgd_dtype xdt, int64_t rows, in
     ranges.add(codes, codes_bytes(rows, cols), true, "codes");
     ranges.add(scales, scales_bytes(rows, cols, 1), true, "scales");
     LSGD_TRY(ranges.check());
-    // a wave per 512 columns while that does not fill the card four times, then one for four
+    // bfloat16: a wave per 512 columns while that does not fill the card four times, then one for four
     const int64_t groups = ceil_div(cols, 512), full = 4 * 32 * static_cast<int64_t>(device_cus());
-    const int64_t across = std::min<int64_t>(1024, rows * groups <= full ? groups : ceil_div(groups, 4));
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(kMaxGridBlocks / across, ceil_div(rows, kBlock / 64))),
-                    static_cast<unsigned>(across));
+    const int64_t of_rows = ceil_div(rows, kBlock / 64);
+    const int64_t across = std::min<int64_t>(1024, xdt == LSGD_F32 || rows * groups <= full ? groups : ceil_div(groups, 4));
+    const dim3 grid = xdt == LSGD_F32
+                          ? dim3(static_cast<unsigned>(across), static_cast<unsigned>(std::min<int64_t>(65535, of_rows)))
+                          : dim3(static_cast<unsigned>(std::min<int64_t>(kMaxGridBlocks / across, of_rows)),
+                                 static_cast<unsigned>(across));
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (xdt == LSGD_F32)
         hipLaunchKernelGGL((quant_rows_kernel<float>), grid, dim3(kBlock), 0, s, static_cast<const float*>(x), rows,

@@ -284,7 +284,7 @@ def guarded8(rows, cols, block):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 127), (5, 128), (7, 129), (2, 511), (4, 513), (33, 1999), (1, 8192)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 127), (5, 128), (7, 129), (2, 511), (4, 513), (33, 1999), (1, 8192), (2, 524801), (270000, 3), (5000, 4000)])
 def test_quant8(dtype, rows, cols):
     x = randn(rows, cols, seed=rows + cols) * torch.exp(3 * randn(rows, cols, seed=9))
     x = x.to(dtype)
