@@ -130,12 +130,9 @@ LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t c
  * else LSGD_ERR_UNSUPPORTED; k at most 2^23); out: m x n of dtype odt. With activations a and
  * parameters b: a layer's output; with an output gradient a and transposed
  * parameters b: the gradient of its input.
- * odt LSGD_F32: products exact, sums in binary32 (matrix instructions on
+ * Products are exact, sums binary32, rounded once to odt (matrix instructions on
  * bfloat16, which holds every element between 2^-126 and 2^128 exactly;
- * smaller ones may count as 0). odt LSGD_BF16: matrix instructions on the 8-bit
- * codes, at twice the rate, which add groups of 8 neighbouring products
- * aligned to the largest of them and drop what lies more than 12 bits below
- * it; the sum goes on in binary32 and is rounded once to bfloat16.
+ * smaller ones may count as 0).
  * k == 0 gives 0. No-op where m or n is 0. Errors as lsgd_embed_lookup.
  */
 LSGD_API lsgd_status lsgd_matmul8(const void* a, const void* a_scales, int32_t a_block, int64_t m,

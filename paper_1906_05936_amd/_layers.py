@@ -223,8 +223,8 @@ def _operand8(codes, scales, what, device=None):
 def matmul8(a, a_scales, b, b_scales, out, stream=None):
     """lsgd_matmul8: out[i][j] = sum over c of a[i][c] * b[j][c], for 8-bit
     matrices a (m rows) and b (n rows) of the same pitch (block 1 or 128, by
-    their scales' number); out: m by n, float32 (exact products) or bfloat16
-    (the faster matrix instructions)."""
+    their scales' number); out: m by n, float32 or bfloat16 (exact products and
+    float32 sums for both)."""
     target = _native_target(a, stream)
     if target is not None:
         st = _lib._marshal.matmul8(a, a_scales, b, b_scales, out, *target)

@@ -17,10 +17,10 @@ struct Operand {
 // 16) outputs, 128 columns of a and b at a time, which the next step's loads
 // (straight into LDS, no registers) overlap. LDS rows are 128 bytes, their
 // 16-byte chunks exchanged by row / 2 % 8, so that the same chunk of 16 rows lies in
-// all 64 banks (by row % 8 two rows of 16 met in each bank, and the kernel below
-// took 215 us instead of 209). b is the matrix instruction's first operand: a lane then holds
-// 4 neighbouring columns of one output row. Offsets inside a tile are 32-bit.
-template <int TM, int TN, int WM, int WN, bool Exact, typename OT>
+// all 64 banks (by row % 8 two rows of 16 met in each bank). b is the matrix
+// instruction's first operand: a lane then holds 4 neighbouring columns of one output
+// row. Offsets inside a tile are 32-bit.
+template <int TM, int TN, int WM, int WN, typename OT>
 __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
                                                                TileOrder order, OT* __restrict__ out) {
     constexpr int kWaves = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, kStage = (BM + BN) * 128;
@@ -89,16 +89,14 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
                 f.half[1] = *reinterpret_cast<const u32x4*>(t + (off ^ 64));
                 return f;
             };
-            using Frag = typename Product<Exact>::Fragment;
-            Frag fb[TN];
+            Widened32 fb[TN];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = Product<Exact>::template prepare<u>(fragment(at_b + j * 2048), wb[j]);
+            for (int j = 0; j < TN; ++j) fb[j] = widen32<u>(fragment(at_b + j * 2048), wb[j]);
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
-                const Frag fa = Product<Exact>::template prepare<u>(fragment(at_a + i * 2048), wa[i]);
+                const Widened32 fa = widen32<u>(fragment(at_a + i * 2048), wa[i]);
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    acc[i][j] = Product<Exact>::template multiply<u>(fb[j], wb[j], fa, wa[i], acc[i][j]);
+                for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[j], fa, acc[i][j]);
             }
         });
     }
@@ -116,17 +114,15 @@ __global__ __launch_bounds__(WM * WN * 64) void matmul8_kernel(Operand A, Operan
 }
 
 // The kernel for many tiles: 256 x 256 outputs in four waves of 128 x 128, one on
-// each SIMD, so that a wave's fragments (64 columns of a and b at a time, for
-// instructions of 32 x 32 x 64) are read while the products of the ones before
-// them run: both live in registers, beside the 256 of the outputs. A stage (128
-// columns of a and b) is in LDS for the fragment reads while the next one
-// arrives. A workgroup goes through several tiles, and its loads run two
-// stages ahead, across the end of a tile: the next one's first stages arrive
-// while this one's outputs leave. 8192 x 8192 x 4096: 209 to 217 us, 2.5 to 2.6
-// PFLOP/s; the matrix units are busy for two thirds of the cycles, at a clock that
-// the power they take brings down to 1.9 GHz. Exact: a wave widens the fragments by
-// quarters (for instructions of 32 x 32 x 16), one while the one before it is
-// multiplied: 386 us, 1.42 PFLOP/s (128 x 128 outputs 495).
+// each SIMD, so that a wave's fragments (64 columns of a and b at a time) are read
+// while the products of the ones before them run, and widened by quarters (for
+// instructions of 32 x 32 x 16), one while the one before it is multiplied: all live
+// in registers, beside the 256 of the outputs. A stage (128 columns of a and b) is in
+// LDS for the fragment reads while the next one arrives. A workgroup goes through
+// several tiles, and its loads run two stages ahead, across the end of a tile: the
+// next one's first stages arrive while this one's outputs leave. 8192 x 8192 x 4096:
+// 349 us to bfloat16, 1.58 PFLOP/s, 367 to binary32 (with 128 x 128 outputs 456, 471):
+// as fast as a large library product of bfloat16, so bound by the matrix units.
 constexpr int kWideTile = 256;
 
 // The stage that a workgroup loads next: tile, place in it, addresses. The last
@@ -164,8 +160,7 @@ struct WideLoads {
         (q < kLoads ? codes_a : codes_b).load_lds16(from, stage * 128 + q % kLoads * 32 * pitch, to + (q * 4 + wave) * 1024);
     }
     // A word holds a row's scales of four stages. It is loaded for the first of them;
-    // for the others the offsets lie outside the buffer, which costs no access (a byte a
-    // stage, for 32 rows at a time: 230 us instead of 215).
+    // for the others the offsets lie outside the buffer, which costs no access.
     __device__ __forceinline__ bool first_of_four() const { return stage % 4 == 0; }
     __device__ __forceinline__ void fetch_scales(int i, uint32_t (&words)[4]) const {
         words[i] = (i < 2 ? scales_a : scales_b).load4((i < 2 ? row_a[i] : row_b[i - 2]) | (first_of_four() ? 0 : 0x80000000u), stage);
@@ -178,7 +173,7 @@ struct WideLoads {
     }
 };
 
-template <bool Exact, typename OT>
+template <typename OT>
 __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
                                                            TileOrder order, OT* __restrict__ out) {
     constexpr int kStage = WideLoads::kStage;
@@ -205,9 +200,9 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
     const uint32_t at = lane % 32 * 128 + ((lane / 32) ^ (lane / 2 % 8)) * 16;
     // the q-th of a half stage's 16 reads
     auto read = [&](Fragments& f, uint32_t stage, int h, auto q) {
-        constexpr int i = Exact ? q % 4 : q / 2 % 4, part = Exact ? q / 8 : q % 2;
+        constexpr int i = q % 4, part = q / 8;
         const uint8_t* x = lds + stage + (at ^ (h * 64 + part * 32));
-        if constexpr (Exact ? q % 8 < 4 : q < 8) f.b[i].half[part] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
+        if constexpr (q % 8 < 4) f.b[i].half[part] = *reinterpret_cast<const u32x4*>(x + (kWideTile + wn + i * 32) * 128);
         else f.a[i].half[part] = *reinterpret_cast<const u32x4*>(x + (wm + i * 32) * 128);
     };
     loads.fetch_all(lds, from, pitch, wave, words);
@@ -217,7 +212,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
     loads.stage = 1;
     loads.fetch_all(lds + kStage, from, pitch, wave, words);
     unrolled<16>([&](auto q) { read(even, 0, 0, q); });
-    // Exact: a quarter of a half stage in bfloat16 (a lane's 8 columns of every row), and
+    // a quarter of a half stage in bfloat16 (a lane's 8 columns of every row), and
     // the next one, whose e-th of 32 steps this is
     struct Widened {
         uint32_t a[4][4], b[4][4];
@@ -228,7 +223,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
         if constexpr (e % 8 < 4) quarter[g % 2].a[i][e % 4] = widen2<e % 2>(f.a[i].word[word], sa);
         else quarter[g % 2].b[i][e % 4] = widen2<e % 2>(f.b[i].word[word], sb);
     };
-    if constexpr (Exact) unrolled<32>([&](auto e) { widen(even, scales, std::integral_constant<int, 0>{}, e); });
+    unrolled<32>([&](auto e) { widen(even, scales, std::integral_constant<int, 0>{}, e); });
     uint32_t here = 0;
     bool four = false;   // whether `words` holds four stages' scales, and not nothing
     for (;;) {
@@ -239,12 +234,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-        auto multiply = [&](const Fragments& f, auto q) {
-            constexpr int i = q / 4, j = q % 4;
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f.b[j].all, f.a[i].all, acc[i][j], 0, 0, 0,
-                                                                       scales[4 + j], 0, scales[i]);
-        };
-        // Exact: a half stage, 64 products of 32 x 32 x 16. Meanwhile the next half is read
+        // a half stage, 64 products of 32 x 32 x 16. Meanwhile the next half is read
         // and, by quarters, widened (`then`: its scales).
         auto half = [&](const Fragments& f, Fragments& next, uint32_t stage, int h, const uint32_t (&then)[8], auto fetch) {
             unrolled<4>([&](auto g) {
@@ -278,17 +268,10 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
             }
 #pragma unroll 1
             for (uint32_t t = last_two ? stages - 2 : 0; t < (last_two ? stages : stages - 2); ++t) {
-                // The order is the source's: a product, a read and a load at a time. (The
-                // compiler put the loads in one burst, and moves of scales behind it, which
-                // waited for them: 243 us instead of 230. Two loads at a time 231, as they
-                // take 16 cycles of the compute unit's 64 a product.)
-                if constexpr (Exact)
-                    half(even, odd, here, 1, scales, [](auto) {});
-                else unrolled<16>([&](auto q) {
-                    multiply(even, q);
-                    read(odd, here, 1, q);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
+                // The order is the source's: a product, then a part of the next quarter's
+                // widening, a read or a load. (The compiler puts the loads in one burst, and
+                // moves of scales behind it, which wait for them.)
+                half(even, odd, here, 1, scales, [](auto) {});
                 loads_done();   // this stage is in every wave's registers, and the next has arrived
                 uint32_t then[8];   // the next stage's scales
 #pragma unroll
@@ -300,17 +283,9 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
                 }
                 ++loads.stage;
                 four = loads.first_of_four();
-                if constexpr (Exact)
-                    half(odd, even, here ^ kStage, 0, then, [&](auto q) {
-                        loads.fetch(q, lds + here, from, pitch, wave);
-                        if constexpr (q < 4) loads.fetch_scales(q, words);
-                    });
-                else unrolled<16>([&](auto q) {
-                    multiply(odd, q);
-                    read(even, here ^ kStage, 0, q);
+                half(odd, even, here ^ kStage, 0, then, [&](auto q) {
                     loads.fetch(q, lds + here, from, pitch, wave);
                     if constexpr (q < 4) loads.fetch_scales(q, words);
-                    __builtin_amdgcn_sched_barrier(0);
                 });
 #pragma unroll
                 for (int i = 0; i < 8; ++i) scales[i] = then[i];
@@ -337,7 +312,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
                     uint8_t* row = mine + l % 32 * 256;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        if constexpr (Exact)
+                        if constexpr (sizeof(OT) == 4)
                             *reinterpret_cast<f32x4*>(row + ((u * 8 + r * 2 + l / 32) ^ (l % 16)) * 16) =
                                 f32x4{v[r * 4], v[r * 4 + 1], v[r * 4 + 2], v[r * 4 + 3]};
                         else
@@ -373,7 +348,7 @@ __global__ __launch_bounds__(256) void matmul8_wide_kernel(Operand A, Operand B,
 // do; loads straight into registers, 64 bytes of a row each, were slower by half),
 // so nothing waits for another wave until the sums meet in LDS, added in wave
 // order.
-template <int TM, int TN, int W, int D, bool Exact, typename OT>
+template <int TM, int TN, int W, int D, typename OT>
 __global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Operand B, uint32_t pitch, uint32_t spitch,
                                                                 TileOrder order, OT* __restrict__ out) {
     constexpr int kSlot = (TM + TN) * 2048, kLoads = (TM + TN) * 2;   // loads of 8 rows each
@@ -430,7 +405,6 @@ __global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Opera
                     f.half[1] = *reinterpret_cast<const u32x4*>(ring + d * kSlot + (off ^ 64));
                     return f;
                 };
-                using Frag = typename Product<Exact>::Fragment;
                 Codes32 ra[TM], rb[TN];
 #pragma unroll
                 for (int j = 0; j < TN; ++j) rb[j] = fragment((TM + j) * 2048 + at);
@@ -443,15 +417,14 @@ __global__ __launch_bounds__(W * 64) void matmul8_narrow_kernel(Operand A, Opera
                 for (int j = 0; j < TN; ++j) vb[j] = wb[d][j];
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read before the slot is loaded again
                 fetch(base + d + D, d);
-                Frag fb[TN];
+                Widened32 fb[TN];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) fb[j] = Product<Exact>::template prepare<0>(rb[j], vb[j]);
+                for (int j = 0; j < TN; ++j) fb[j] = widen32<0>(rb[j], vb[j]);
 #pragma unroll
                 for (int i = 0; i < TM; ++i) {
-                    const Frag fa = Product<Exact>::template prepare<0>(ra[i], va[i]);
+                    const Widened32 fa = widen32<0>(ra[i], va[i]);
 #pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        acc[i][j] = Product<Exact>::template multiply<0>(fb[j], vb[j], fa, va[i], acc[i][j]);
+                    for (int j = 0; j < TN; ++j) acc[i][j] = multiply(fb[j], fa, acc[i][j]);
                 }
             });
     }
@@ -477,26 +450,26 @@ __global__ __launch_bounds__(kBlock) void zero_kernel(OT* __restrict__ out, int6
         out[i] = 0;
 }
 
-template <int TM, int TN, int WM, int WN, bool Exact, typename OT>
+template <int TM, int TN, int WM, int WN, typename OT>
 lsgd_status launch_tiles(const Operand& a, const Operand& b, int64_t k, void* out, hipStream_t s) {
     const TileOrder order(ceil_div(a.rows, WM * TM * 16), ceil_div(b.rows, WN * TN * 16));
     if (order.blocks() > kMaxGridBlocks) return fail(LSGD_ERR_SIZE, "%lld tiles", static_cast<long long>(order.blocks()));
-    hipLaunchKernelGGL((matmul8_kernel<TM, TN, WM, WN, Exact, OT>), dim3(static_cast<unsigned>(order.blocks())),
+    hipLaunchKernelGGL((matmul8_kernel<TM, TN, WM, WN, OT>), dim3(static_cast<unsigned>(order.blocks())),
                        dim3(WM * WN * 64), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
                        static_cast<uint32_t>(scale_pitch8(k)), order, static_cast<OT*>(out));
     return check_launch("lsgd_matmul8");
 }
 
-template <int TM, int TN, int W, int D, bool Exact, typename OT>
+template <int TM, int TN, int W, int D, typename OT>
 lsgd_status launch_narrow(const Operand& a, const Operand& b, int64_t k, void* out, hipStream_t s) {
     const TileOrder order(ceil_div(a.rows, TM * 16), ceil_div(b.rows, TN * 16));
-    hipLaunchKernelGGL((matmul8_narrow_kernel<TM, TN, W, D, Exact, OT>), dim3(static_cast<unsigned>(order.blocks())), dim3(W * 64),
+    hipLaunchKernelGGL((matmul8_narrow_kernel<TM, TN, W, D, OT>), dim3(static_cast<unsigned>(order.blocks())), dim3(W * 64),
                        0, s, a, b, static_cast<uint32_t>(pitch8(k)), static_cast<uint32_t>(scale_pitch8(k)), order,
                        static_cast<OT*>(out));
     return check_launch("lsgd_matmul8");
 }
 
-template <bool Exact, typename OT>
+template <typename OT>
 lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hipStream_t s) {
     if (k == 0) {
         const int64_t n = a.rows * b.rows;
@@ -505,38 +478,38 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
         return check_launch("lsgd_matmul8");
     }
     // The smallest tile of which every compute unit gets at most one: with one
-    // round of workgroups the time is a wave's loads one after another. us, at
+    // round of workgroups the time is a wave's loads one after another. us to bfloat16, at
     // m x n x k, 16x16 / 32x16 / 32x32 / 64x32 / 64x64 / 128x128 outputs:
-    // 16x4096x4096 5.3 / 6.2 / 7.1 / 8.0 / 10.8 / 20.9, 256x512x4096 8.2 / 7.4 / 8.4 /
-    // 11.2 / 13.5 / 25.1, 512x512x512 5.2 / 5.2 / 4.2 / 4.3 / 6.2 / 6.4, 256x2048x2048
-    // 15.8 / 15.7 / 10.0 / 6.9 / 8.9 / 13.9, 1024x1024x4096 50 / 49 / 29 / 21 / 14 / 28
-    // (about 4 of each is the call).
+    // 16x4096x4096 5.3 / 6.3 / 7.1 / 8.7 / 12.8 / 35, 256x512x4096 8.3 / 7.5 / 8.3 /
+    // 11.7 / 15.0 / 40, 512x512x512 5.2 / 5.2 / 4.0 / 4.5 / 6.3 / 8.3, 256x2048x2048
+    // 15.9 / 15.6 / 10.0 / 7.0 / 9.7 / 21, 1024x1024x4096 46 / 49 / 29 / 22 / 16 / 41
+    // (about 4 of each is the call; to binary32 the same).
     const auto fits = [&](int64_t rows, int64_t cols) {
         return ceil_div(a.rows, rows) * ceil_div(b.rows, cols) <= device_cus();
     };
-    if (fits(16, 16)) return launch_narrow<1, 1, 8, 2, Exact, OT>(a, b, k, out, s);
-    if (fits(32, 16)) return launch_narrow<2, 1, 8, 2, Exact, OT>(a, b, k, out, s);
-    if (fits(32, 32)) return launch_narrow<2, 2, 8, 2, Exact, OT>(a, b, k, out, s);
-    if (fits(64, 32)) return launch_narrow<4, 2, 8, 1, Exact, OT>(a, b, k, out, s);
-    // On bfloat16 a stage of 128 x 128 outputs takes twice as long, and two rounds of
-    // 64 x 64 are faster where there are many: us, 64 x 64 / 128 x 128: 1792x848x2804 23 / 28,
-    // 166x6658x2723 22 / 28, 1402x951x1610 18 / 18, 794x1835x724 13 / 11.
-    const bool two_rounds = Exact && k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * device_cus();
-    if (fits(64, 64) || two_rounds) return launch_narrow<4, 4, 4, 2, Exact, OT>(a, b, k, out, s);
+    if (fits(16, 16)) return launch_narrow<1, 1, 8, 2, OT>(a, b, k, out, s);
+    if (fits(32, 16)) return launch_narrow<2, 1, 8, 2, OT>(a, b, k, out, s);
+    if (fits(32, 32)) return launch_narrow<2, 2, 8, 2, OT>(a, b, k, out, s);
+    if (fits(64, 32)) return launch_narrow<4, 2, 8, 1, OT>(a, b, k, out, s);
+    // Two rounds of 64 x 64 outputs are faster than one of 128 x 128 where many columns
+    // are summed: us, 64 x 64 / 128 x 128: 1792x848x2804 23 / 28, 166x6658x2723 22 / 27,
+    // 1402x951x1610 18 / 19, 794x1835x724 13 / 12.
+    const bool two_rounds = k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * device_cus();
+    if (fits(64, 64) || two_rounds) return launch_narrow<4, 4, 4, 2, OT>(a, b, k, out, s);
     // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
-    // compute unit, which hold half of it: k = 4096, us, wide / 128 x 128: 2048x4096
-    // 43 / 41, 2304x4096 44 / 61, 4096x4096 57 / 78, 4608x4096 93 / 97, 6144x4096
-    // 97 / 116, 8192x8192 217 / 302; Exact 70 / 65, 73 / 94, 104 / 127, 163 / 152,
-    // 172 / 192, 386 / 495.
+    // compute unit, which hold half of it: k = 4096, us to bfloat16, wide / 128 x 128:
+    // 2048x4096 67 / 62, 2304x4096 69 / 91, 4096x4096 90 / 118, 4608x4096 151 / 143,
+    // 6144x4096 152 / 174, 8192x8192 349 / 456 (to binary32 69 / 63, 70 / 91, 98 / 120,
+    // 156 / 145, 157 / 176, 367 / 471).
     const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
     const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
     if (a.rows >= kWideTile && b.rows >= kWideTile && k > 128 && ceil_div(wide.tiles(), 256) < ceil_div(tiles, 512)) {
         const dim3 grid(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8)));
-        hipLaunchKernelGGL((matmul8_wide_kernel<Exact, OT>), grid, dim3(256), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
+        hipLaunchKernelGGL((matmul8_wide_kernel<OT>), grid, dim3(256), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
                            static_cast<uint32_t>(scale_pitch8(k)), wide, static_cast<OT*>(out));
         return check_launch("lsgd_matmul8");
     }
-    return launch_tiles<4, 4, 2, 2, Exact, OT>(a, b, k, out, s);
+    return launch_tiles<4, 4, 2, 2, OT>(a, b, k, out, s);
 }
 
 }  // namespace
@@ -579,7 +552,7 @@ LSGD_API lsgd_status lsgd_matmul8(const void* a, const void* a_scales, int32_t a
     const Operand A{static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(a_scales), m, a_block == 1 ? 0 : 7};
     const Operand B{static_cast<const uint8_t*>(b), static_cast<const uint8_t*>(b_scales), n, b_block == 1 ? 0 : 7};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return odt == LSGD_F32 ? launch<true, float>(A, B, k, out, s) : launch<false, uint16_t>(A, B, k, out, s);
+    return odt == LSGD_F32 ? launch<float>(A, B, k, out, s) : launch<uint16_t>(A, B, k, out, s);
 }
 
 }  // extern "C"

@@ -8,7 +8,6 @@
 namespace lsgd {
 namespace layers {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -119,7 +118,6 @@ __device__ __forceinline__ void lds_done() {
 // 32 codes of one row: a lane's part of 128 columns.
 union Codes32 {
     u32x4 half[2];
-    i32x8 all;
     uint32_t word[8];
 };
 
@@ -135,52 +133,32 @@ __device__ __forceinline__ u32x2 widen4(uint32_t codes, float scale) {
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
-// acc + x y^T over 128 columns of 16 rows each; word `U`'s byte of a lane's
-// scale word is that of its row. Which columns a lane holds does not matter, as
-// long as both sides hold the same ones.
-template <bool Exact>
-struct Product;
-
-// On the codes: the instruction multiplies by the scales.
-template <>
-struct Product<false> {
-    using Fragment = i32x8;
-    template <int U>
-    static __device__ __forceinline__ Fragment prepare(const Codes32& c, uint32_t) {
-        return c.all;
-    }
-    template <int U>
-    static __device__ __forceinline__ f32x4 multiply(const Fragment& x, uint32_t sx, const Fragment& y, uint32_t sy,
-                                                     f32x4 acc) {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, acc, 0, 0, U, sx, U, sy);
-    }
+// The 32 codes times the scale in byte U of the lane's scale word (that of its row).
+struct Widened32 {
+    bf16x8 part[4];
 };
+template <int U>
+__device__ __forceinline__ Widened32 widen32(const Codes32& c, uint32_t scales) {
+    const float s = scale_value(scales >> (8 * U) & 0xffu);
+    Widened32 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u32x2 a = widen4(c.word[2 * i], s), b = widen4(c.word[2 * i + 1], s);
+        f.part[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
+    }
+    return f;
+}
 
-// On bfloat16: each product exact, binary32 sums.
-template <>
-struct Product<true> {
-    struct Fragment {
-        bf16x8 part[4];
-    };
-    template <int U>
-    static __device__ __forceinline__ Fragment prepare(const Codes32& c, uint32_t scales) {
-        const float s = scale_value(scales >> (8 * U) & 0xffu);
-        Fragment f;
+// acc + x y^T over 128 columns of 16 rows each, each product exact, binary32 sums. Which
+// columns a lane holds does not matter, as long as both sides hold the same ones. (The
+// instructions on the codes themselves have twice the rate, but add groups of 8 products
+// aligned to the largest of them and drop what lies more than 12 bits below it: 448 * 448 -
+// 448 * 448 + 1 gives 0.)
+__device__ __forceinline__ f32x4 multiply(const Widened32& x, const Widened32& y, f32x4 acc) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const u32x2 a = widen4(c.word[2 * i], s), b = widen4(c.word[2 * i + 1], s);
-            f.part[i] = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
-        }
-        return f;
-    }
-    template <int U>
-    static __device__ __forceinline__ f32x4 multiply(const Fragment& x, uint32_t, const Fragment& y, uint32_t,
-                                                     f32x4 acc) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.part[i], y.part[i], acc, 0, 0, 0);
-        return acc;
-    }
-};
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.part[i], y.part[i], acc, 0, 0, 0);
+    return acc;
+}
 
 __device__ __forceinline__ float value_of(float x) { return x; }
 __device__ __forceinline__ float value_of(uint16_t x) { return bf16_to_f32(x); }

@@ -422,6 +422,26 @@ def test_matmul8_whole_numbers_and_their_places(odt, m, n, k):
 
 
 @pytest.mark.parametrize("odt", [F32, BF16])
+@pytest.mark.parametrize("m,n,k", [(3, 20, 300), (150, 140, 300), (600, 600, 140), (1200, 2100, 300), (2200, 4003, 300)])
+def test_matmul8_small_terms_beside_large_ones_that_cancel(odt, m, n, k):
+    """Pairs of products of 448 * 448 that cancel, among products of 1: all are whole
+    numbers and every partial sum stays below 2^24, so that binary32 sums are exact in
+    any order, and outputs below 256 are exact in bfloat16 too."""
+    a, b = randint(m * k, -1, 2, seed=1).view(m, k).float(), randint(n * k, -1, 2, seed=2).view(n, k).float()
+    a *= torch.arange(k, device=DEV) % 2
+    places = torch.randperm(k, generator=torch.Generator().manual_seed(3))[:32].to(DEV)
+    signs = randint(m * 16, 0, 2, seed=4).view(m, 16) * 2.0 - 1
+    a[:, places] = torch.cat([signs, -signs], 1) * 448
+    b[:, places] = (randint(n * 16, 0, 2, seed=5).view(n, 16) * 2.0 - 1).repeat(1, 2) * 448
+    (qa, sa), (qb, sb) = as8(a, 1), as8(b, 128)
+    assert torch.equal(values(qa, sa, 1, k), a.double()) and torch.equal(values(qb, sb, 128, k), b.double())
+    out = nans(m, n, dtype=odt)
+    lsgd.matmul8(qa, sa, qb, sb, out)
+    want = a.double() @ b.double().t().contiguous()
+    assert 16 < want.abs().max() < 256 and torch.equal(out.double(), want)
+
+
+@pytest.mark.parametrize("odt", [F32, BF16])
 def test_matmul8_scales_at_their_ends(odt):
     """Elements near 2^100 against elements near 2^-100: the scales meet in
     binary32's range though neither lies near 1."""
