@@ -701,7 +701,7 @@ lsgd_status sort_tokens(const Workers& w, uint32_t n_tokens, uint32_t E, uint32_
     const unsigned blocks = static_cast<unsigned>(sort_blocks(E));
     uint32_t *counts = u32(l.counts), *totals = blocks > kOwnSums ? u32(l.totals) : nullptr;
     int from = 0;
-    for (int shift = 0; shift == 0 || rows >> shift; shift += kDigitBits) {   // keys reach `rows`
+    for (int shift = 0; shift == 0 || (shift < 32 && rows >> shift); shift += kDigitBits) {   // keys reach `rows`
         const uint32_t *key = u32(l.key[from]), *entry = u32(l.entry[from]);
         uint32_t *key_out = u32(l.key[1 - from]), *entry_out = u32(l.entry[1 - from]);
         if (shift == 0)

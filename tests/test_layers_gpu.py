@@ -162,6 +162,24 @@ def test_grad(gdt, odt, rows, dim, n, workers, it, how):
         assert torch.equal(again[:rows], buf[:rows])
 
 
+@pytest.mark.parametrize("rows", [(1 << 27) + 5, (1 << 31) - 1])
+def test_grad_of_a_table_whose_rows_take_every_digit(rows):
+    """Tokens that differ in their highest bits, in their lowest, or lie outside (whole
+    numbers: exact)."""
+    n = 9001
+    low, high = randint(n, 0, 6, seed=1), randint(n, 0, 1 + rows // (1 << 27), seed=2) * (1 << 27)
+    tokens = torch.where(randint(n, 0, 4, seed=3) > 0, low + high, randint(n, 0, rows + 1, seed=4))
+    tokens[::7], tokens[3::7] = -1, rows
+    tokens[5], tokens[8] = rows - 1, 0
+    g = randint(n, -8, 9, seed=5).float().view(n, 1)
+    want = torch.zeros(rows, 1, device=DEV)
+    inside = (tokens >= 0) & (tokens < rows)
+    want.index_add_(0, tokens[inside], g[inside])
+    out = nans(rows, 1)
+    lsgd.embed_grad([g], [tokens], out)
+    assert torch.equal(out, want)
+
+
 def test_grad_no_tokens():
     none = torch.empty(0, dtype=torch.int64, device=DEV)
     out = nans(5, 9)

@@ -1,0 +1,81 @@
+"""The launches that the layer operators make, on the host: a program that links
+liblsgd.so and defines the HIP runtime's launch itself records every grid
+instead of running it, so that sizes beyond any card's memory can be asked for."""
+import os
+import subprocess
+
+import pytest
+
+from paper_1906_05936_amd.build import INCLUDE, LIB
+
+MAIN = r"""
+#include <stdint.h>
+#include <stdio.h>
+#include <stdlib.h>
+#include <string.h>
+#include "layers/lsgd_layers.h"
+
+typedef struct { uint32_t x, y, z; } dim3;
+static dim3 grid, block;
+static int launches;
+int __hipPushCallConfiguration(dim3 g, dim3 b, size_t shared, void* stream) {
+    (void)shared, (void)stream;
+    grid = g, block = b;
+    return 0;
+}
+int __hipPopCallConfiguration(dim3* g, dim3* b, size_t* shared, void** stream) {
+    *g = grid, *b = block, *shared = 0, *stream = NULL;
+    return 0;
+}
+int hipLaunchKernel(const void* f, dim3 g, dim3 b, void** args, size_t shared, void* stream) {
+    (void)f, (void)args, (void)shared, (void)stream;
+    ++launches;
+    printf("%u %u %u %u %u %u\n", g.x, g.y, g.z, b.x, b.y, b.z);
+    return 0;
+}
+int hipGetLastError(void) { return 0; }
+int hipPeekAtLastError(void) { return 0; }
+int hipGetDevice(int* d) { return *d = 0; }
+int hipDeviceGetAttribute(int* v, int a, int d) { (void)a, (void)d; *v = 256; return 0; }
+
+static void* at(int k) { return (void*)((uintptr_t)k << 42); }   /* buffers far apart, read by nobody */
+
+int main(int argc, char** argv) {
+    int64_t v[8] = {0};
+    for (int i = 2; i < argc; ++i) v[i - 2] = atoll(argv[i]);
+    int st = -1;
+    if (!strcmp(argv[1], "embed_grad")) {   /* tokens, rows, dim */
+        const void *g = at(1), *t = at(2);
+        size_t bytes;
+        lsgd_embed_grad_workspace_size(1, v[0], v[1], v[2], &bytes);
+        st = lsgd_embed_grad(&g, LSGD_F32, &t, LSGD_I64, 1, v[0], v[1], v[2], 1.0f, at(3), LSGD_F32, 0, at(4), bytes, NULL);
+    }
+    return st;
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def launches(tmp_path_factory):
+    d = tmp_path_factory.mktemp("launches")
+    (d / "main.c").write_text(MAIN)
+    exe, lib_dir = str(d / "main"), os.path.dirname(LIB)
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-rdynamic", "-I" + INCLUDE, str(d / "main.c"), "-o", exe,
+                    "-L" + lib_dir, "-llsgd", "-Wl,-rpath," + lib_dir], check=True)
+
+    def run(*args):
+        """[(grid, block)] of a call, each of whose launches has to fit a dispatch."""
+        out = subprocess.run([exe] + [str(x) for x in args], capture_output=True, text=True, check=True, timeout=60).stdout
+        got = [tuple(map(int, line.split())) for line in out.splitlines()]
+        for g in got:
+            assert all(n > 0 and n * b < 1 << 32 for n, b in zip(g[:3], g[3:])), g
+        return [(g[:3], g[3:]) for g in got]
+    return run
+
+
+@pytest.mark.parametrize("rows,passes", [(511, 1), (512, 2), ((1 << 18) - 1, 2), (1 << 18, 3), ((1 << 27) - 1, 3),
+                                         (1 << 27, 4), ((1 << 31) - 1, 4)])
+def test_sort_passes(launches, rows, passes):
+    """9 bits of the key a pass, keys up to `rows`: two launches a pass, then the rows'
+    ends, the sums and the joins."""
+    assert len(launches("embed_grad", 9000, rows, 1)) == 2 * passes + 3
