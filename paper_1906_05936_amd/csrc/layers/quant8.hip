@@ -91,8 +91,10 @@ __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict_
 // transposed: 32 us, 6.3 TB/s; with stores through the caches 47), and where the
 // tiles are few by the way from load to store (1000 x 777: 4.9 us; with four 4 x 4 to
 // each of a quarter of the lanes 7.3, and 33 for the large one). Up to kCopies copies
-// a launch keep their pointers in the kernel's arguments.
+// a launch keep their pointers in the kernel's arguments; up to kLaunchTiles tiles
+// side by side fit a launch, the next one starts at first_col.
 constexpr int kTileThreads = 1024;
+constexpr int64_t kLaunchTiles = 0xffffffffLL / kTileThreads;   // a dispatch holds at most 2^32 - 1 work-items along x
 constexpr int kCopies = 32;
 constexpr int kRowWords = 33;    // LDS words per row of 128 codes: rows start in different banks
 
@@ -119,11 +121,11 @@ __device__ __forceinline__ void put_tile(const uint32_t (&tile)[128][kRowWords],
 }
 
 __global__ __launch_bounds__(kTileThreads) void quant_blocks_kernel(const float* __restrict__ p, int64_t rows,
-                                                                    int64_t cols, Copies plain, int n_plain,
-                                                                    Copies transposed, int n_transposed) {
+                                                                    int64_t cols, int64_t first_col, Copies plain,
+                                                                    int n_plain, Copies transposed, int n_transposed) {
     __shared__ uint32_t tile[128][kRowWords];
     __shared__ float wave_max[kTileThreads / 64];
-    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 128, r0 = static_cast<int64_t>(blockIdx.y) * 128;
+    const int64_t c0 = first_col + static_cast<int64_t>(blockIdx.x) * 128, r0 = static_cast<int64_t>(blockIdx.y) * 128;
     const int tr = threadIdx.x / 32 * 4, tc = threadIdx.x % 32 * 4;
     const int k = static_cast<int>(max(static_cast<int64_t>(0), min(cols - c0 - tc, static_cast<int64_t>(4))));
     float v[4][4];
@@ -242,7 +244,7 @@ LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t c
         ranges.add(scales_t[i], scales_bytes(cols, rows, 128), true, "a transposed replica's scales");
     }
     LSGD_TRY(ranges.check());
-    const dim3 grid(static_cast<unsigned>(ceil_div(cols, 128)), static_cast<unsigned>(ceil_div(rows, 128)));
+    const int64_t tiles = ceil_div(cols, 128);
     for (int32_t at = 0; at < n_replicas || at < n_transposed; at += kCopies) {
         Copies a{}, b{};
         const int na = std::max(0, std::min(kCopies, n_replicas - at));
@@ -251,9 +253,13 @@ LSGD_API lsgd_status lsgd_copy_out8(const float* params, int64_t rows, int64_t c
             a.codes[i] = static_cast<uint8_t*>(codes[at + i]), a.scales[i] = static_cast<uint8_t*>(scales[at + i]);
         for (int i = 0; i < nb; ++i)
             b.codes[i] = static_cast<uint8_t*>(codes_t[at + i]), b.scales[i] = static_cast<uint8_t*>(scales_t[at + i]);
-        hipLaunchKernelGGL(quant_blocks_kernel, grid, dim3(kTileThreads), 0, static_cast<hipStream_t>(stream), params, rows,
-                           cols, a, na, b, nb);
-        LSGD_TRY(check_launch("lsgd_copy_out8"));
+        for (int64_t tile = 0; tile < tiles; tile += kLaunchTiles) {
+            const dim3 grid(static_cast<unsigned>(std::min(kLaunchTiles, tiles - tile)),
+                            static_cast<unsigned>(ceil_div(rows, 128)));
+            hipLaunchKernelGGL(quant_blocks_kernel, grid, dim3(kTileThreads), 0, static_cast<hipStream_t>(stream), params,
+                               rows, cols, tile * 128, a, na, b, nb);
+            LSGD_TRY(check_launch("lsgd_copy_out8"));
+        }
     }
     return LSGD_OK;
 }

@@ -769,6 +769,27 @@ def test_copies_past_32_bits():
     assert torch.equal(copies[1][0][:, first:rows].view(torch.uint8), q.view(torch.uint8)[:, :cols].T)
 
 
+def test_copies_of_more_columns_than_a_launch_takes():
+    cols = (1 << 29) + 1000
+    p, q, s = torch.zeros(2, cols, device=DEV), *lsgd.empty8(2, cols, 128)
+    q.view(torch.uint8).fill_(0x55)
+    s.view(torch.uint8).fill_(0x55)
+    full = (1 << 29) - 128   # columns of the first launch
+    parts = [(0, 1024), (full - 512, full + 512), (full, cols)]
+    for lo, hi in parts:
+        p[:, lo:hi] = randn(2, hi - lo, seed=lo % 7)
+    lsgd.copy_out8(p, [(q, s)])
+    q, s = q.view(torch.uint8), s.view(torch.uint8)
+    for lo, hi in parts:
+        want, scales = lsgd.empty8(2, hi - lo, 128)
+        lsgd.copy_out8(p[:, lo:hi].contiguous(), [(want, scales)])
+        wide = want.shape[1]
+        assert torch.equal(q[:, lo:lo + wide], want.view(torch.uint8))
+        assert torch.equal(s[:, lo // 128:(lo + wide) // 128], scales.view(torch.uint8)[:, :wide // 128])
+    assert torch.count_nonzero(q[:, 1024:full - 512]) == 0 and (s[:, 8:(full - 512) // 128] == 127).all()
+    assert torch.count_nonzero(q[:, cols:]) == 0 and (s[:, -(-cols // 128):] == 127).all()
+
+
 @pytest.mark.parametrize("name", ["gradient", "weights"])
 def test_a_workspace_for_another_stream(name):
     """`stream` names a stream that is not the current one: the workspace that the call

@@ -50,6 +50,10 @@ int main(int argc, char** argv) {
         lsgd_embed_grad_workspace_size(1, v[0], v[1], v[2], &bytes);
         st = lsgd_embed_grad(&g, LSGD_F32, &t, LSGD_I64, 1, v[0], v[1], v[2], 1.0f, at(3), LSGD_F32, 0, at(4), bytes, NULL);
     }
+    if (!strcmp(argv[1], "copy_out8")) {   /* rows, cols */
+        void *q = at(2), *s = at(3);
+        st = lsgd_copy_out8(at(1), v[0], v[1], &q, &s, 1, NULL, NULL, 0, NULL);
+    }
     return st;
 }
 """
@@ -79,3 +83,11 @@ def test_sort_passes(launches, rows, passes):
     """9 bits of the key a pass, keys up to `rows`: two launches a pass, then the rows'
     ends, the sums and the joins."""
     assert len(launches("embed_grad", 9000, rows, 1)) == 2 * passes + 3
+
+
+@pytest.mark.parametrize("cols", [1, 128, 4096, (1 << 29) - 256, (1 << 29) - 255, 1 << 29, (1 << 30) + 7, (1 << 31) - 1])
+def test_copy_out_tiles(launches, cols):
+    """A workgroup for every 128 columns, in as many launches as they need."""
+    got = launches("copy_out8", 300, cols)
+    assert sum(g[0] for g, _ in got) == -(-cols // 128) and all(g[1:] == (3, 1) for g, _ in got)
+    assert len(got) == -(-cols // 128) // ((1 << 32) // 1024) + 1
