@@ -27,10 +27,13 @@ __device__ __forceinline__ float max_of_16(float a) {
 // long as it takes few instructions: fmaxf passes NaNs over, and only where an
 // infinity is left are the magnitudes looked at again. 16384 x 4096 bfloat16: 35 us,
 // 5.8 TB/s; with x kept in the caches, or a wave for every 512 columns, 39 to 42.
-// binary32: 53 us, 6.4 TB/s, with 4 of a lane's columns in either half of the block, so
-// that an instruction reads whole lines, and neighbouring workgroups on the same
-// rows, a wave for every 512 columns; as for bfloat16 75 us, which with rows of
-// odd length is the other way round (8191: 38 us, along the rows 43 to 65).
+// For binary32 a lane has 4 columns in either half of the block, so that an
+// instruction reads whole lines, and neighbouring workgroups take the same rows, a
+// wave for every 512 columns: 16384 x 4096 53 us, 6.4 TB/s, with 8 neighbours a lane and
+// neighbouring workgroups along the rows, as for bfloat16, 75; 16384 x 4095 62 and 71,
+// 8192 x 8191 60 and 69, 333 x 1999 3.2 and 3.4, 5000 x 129 3.9 and 3.6. For bfloat16
+// the order of the workgroups makes 34 of 35 us at 16384 x 4096, but 43 of 38 at 8192 x
+// 8191 and 24 of 21 at 4096 x 8191.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict__ x, int64_t rows, int64_t cols,
                                                             int64_t pitch, int64_t spitch, uint32_t groups,
