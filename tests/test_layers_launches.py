@@ -54,6 +54,30 @@ int main(int argc, char** argv) {
         void *q = at(2), *s = at(3);
         st = lsgd_copy_out8(at(1), v[0], v[1], &q, &s, 1, NULL, NULL, 0, NULL);
     }
+    if (!strcmp(argv[1], "aliases")) {   /* copies, seed: some of them overlap, or none */
+        enum { BYTES = 4096 };   /* 5 x 7 parameters: codes 5 x 128 and 7 x 128, scales 4 and 4 */
+        const int64_t bytes[5] = {140, 5 * 128, 4, 7 * 128, 4};
+        void* p[5][LSGD_MAX_REPLICAS];
+        uint64_t x = (uint64_t)v[1] * 2 + 1;
+        int overlaps = 0, n = (int)v[0];
+        for (int i = 0; i < n; ++i)
+            for (int k = 0; k < 5; ++k) {
+                x = x * 6364136223846793005u + 1442695040888963407u;
+                /* each in a page of its own, or rarely anywhere */
+                uint64_t at = (uint64_t)(i * 5 + k) * BYTES, any = (x >> 33) % ((uint64_t)n * 5 * BYTES);
+                p[k][i] = (char*)0x10000000 + (((x >> 20) % (3 * (uint64_t)n) ? at : any) & ~15ull);
+            }
+        for (int a = 0; a < n * 5; ++a)
+            for (int b = 0; b < a; ++b) {
+                const int ka = a % 5, kb = b % 5, ia = a / 5, ib = b / 5;
+                const char *pa = p[ka][ia], *pb = p[kb][ib];
+                if ((ka == 0 && ia > 0) || (kb == 0 && ib > 0)) continue;   /* one array of parameters */
+                if (pa < pb + bytes[kb] && pb < pa + bytes[ka]) overlaps = 1;
+            }
+        st = lsgd_copy_out8(p[0][0], 5, 7, p[1], p[2], n, p[3], p[4], n, NULL);
+        printf("%d\n", overlaps);
+        return st == (overlaps ? LSGD_ERR_ALIAS : LSGD_OK) && (launches > 0) == !overlaps ? 0 : 100;
+    }
     return st;
 }
 """
@@ -67,9 +91,11 @@ def launches(tmp_path_factory):
     subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-rdynamic", "-I" + INCLUDE, str(d / "main.c"), "-o", exe,
                     "-L" + lib_dir, "-llsgd", "-Wl,-rpath," + lib_dir], check=True)
 
-    def run(*args):
-        """[(grid, block)] of a call, each of whose launches has to fit a dispatch."""
+    def run(*args, text=False):
+        """[(grid, block)] of a call, each of whose launches has to fit a dispatch; or its text."""
         out = subprocess.run([exe] + [str(x) for x in args], capture_output=True, text=True, check=True, timeout=60).stdout
+        if text:
+            return out
         got = [tuple(map(int, line.split())) for line in out.splitlines()]
         for g in got:
             assert all(n > 0 and n * b < 1 << 32 for n, b in zip(g[:3], g[3:])), g
@@ -91,3 +117,10 @@ def test_copy_out_tiles(launches, cols):
     got = launches("copy_out8", 300, cols)
     assert sum(g[0] for g, _ in got) == -(-cols // 128) and all(g[1:] == (3, 1) for g, _ in got)
     assert len(got) == -(-cols // 128) // ((1 << 32) // 1024) + 1
+
+
+@pytest.mark.parametrize("copies", [1, 2, 17, 128])
+def test_aliases_are_found(launches, copies):
+    """Copies that overlap each other or the parameters, against all pairs."""
+    found = {launches("aliases", copies, seed, text=True).split()[-1] for seed in range(40)}
+    assert found == {"0", "1"}   # of both kinds
