@@ -390,11 +390,12 @@ __global__ __launch_bounds__(kBlock) void add_parts_kernel(const float* __restri
 }
 
 // How a call is done: tiles of 256, 128 or 64 outputs each way, and the summed rows
-// in `count` shares whose parts are added at the end.
+// in `count` shares whose parts, where there are several, are added at the end.
 constexpr int64_t kMaxSplit = int64_t{1} << 30;   // outputs: add_parts_kernel's threads stay within a dispatch
 struct Way {
     int tile, count;
     int64_t share;
+    size_t parts_bytes(int64_t n, int64_t k) const { return count > 1 ? static_cast<size_t>(count) * n * k * 4 : 0; }
 };
 
 // The way with the least estimated time. A stage of 64 rows takes 1.7 us of a compute
@@ -406,7 +407,8 @@ struct Way {
 // 2048x4096x1024 56 / 31 / 39, 1024x1024x1024 33 / 18 / 10, 4099x300x515 26 / 15 / 13. With
 // parts at 1.5 bytes a ns they were too few (6000x1000x1000 41 instead of 30).
 Way way_of(int64_t m, int64_t n, int64_t k) {
-    Way best{128, 1, 0};
+    if (m == 0) return Way{128, 1, kStep};
+    Way best{};
     double least = 0;
     const int64_t stages = ceil_div(m, kStep);
     for (int tile = 256; tile >= 64; tile /= 2) {
@@ -418,13 +420,14 @@ Way way_of(int64_t m, int64_t n, int64_t k) {
         };
         const int64_t most = n * k > kMaxSplit ? 1 : std::min<int64_t>(stages, 64);
         for (int64_t count = 1; count <= most; ++count) {
+            const double join_us = count > 1 ? 3 + count * (0.1 + n * k / 0.6e6) : 0;
+            if (best.count > 0 && join_us >= least) break;   // and so for more of them
             const int64_t each = ceil_div(stages, count);
             if (count > 1 && ceil_div(stages, each) != count) continue;
             const int64_t rounds = tiles * count / (cus * most_of_cu), rest = tiles * count - rounds * cus * most_of_cu;
             const double us = rounds * (each * stage_us(most_of_cu) + fixed_us) +
-                              (rest > 0 ? each * stage_us(ceil_div(rest, cus)) + fixed_us : 0) +
-                              (count > 1 ? 3 + count * (0.1 + n * k / 0.6e6) : 0);
-            if (least == 0 || us < least) least = us, best = Way{tile, static_cast<int>(count), each * kStep};
+                              (rest > 0 ? each * stage_us(ceil_div(rest, cus)) + fixed_us : 0) + join_us;
+            if (best.count == 0 || us < least) least = us, best = Way{tile, static_cast<int>(count), each * kStep};
         }
     }
     return best;
@@ -450,9 +453,8 @@ lsgd_status launch_tiles(const Way& w, const void* grad, const void* x, const vo
 }
 
 template <typename OT>
-lsgd_status launch(const void* grad, const void* x, const void* scales, int64_t m, int64_t n, int64_t k, void* out,
-                   bool accumulate, void* workspace, hipStream_t s) {
-    const Way w = m > 0 ? way_of(m, n, k) : Way{128, 1, kStep};
+lsgd_status launch(const Way& w, const void* grad, const void* x, const void* scales, int64_t m, int64_t n, int64_t k,
+                   void* out, bool accumulate, void* workspace, hipStream_t s) {
     float* parts = static_cast<float*>(workspace);
     if (w.tile == 256) LSGD_TRY((launch_tiles<256, OT>(w, grad, x, scales, m, n, k, out, accumulate, parts, s)));
     else if (w.tile == 128) LSGD_TRY((launch_tiles<128, OT>(w, grad, x, scales, m, n, k, out, accumulate, parts, s)));
@@ -478,12 +480,6 @@ lsgd_status check_sizes(int64_t m, int64_t n, int64_t k) {
     return LSGD_OK;
 }
 
-size_t workspace_bytes_of(int64_t m, int64_t n, int64_t k) {
-    if (m == 0 || n == 0 || k == 0) return 0;
-    const Way w = way_of(m, n, k);
-    return w.count > 1 ? static_cast<size_t>(w.count) * n * k * 4 : 0;
-}
-
 }  // namespace
 }  // namespace layers
 }  // namespace lsgd
@@ -496,7 +492,7 @@ extern "C" {
 LSGD_API lsgd_status lsgd_weight_grad8_workspace_size(int64_t m, int64_t n, int64_t k, size_t* bytes) {
     LSGD_TRY(check_sizes(m, n, k));
     if (!bytes) return fail(LSGD_ERR_NULL, "bytes is NULL");
-    *bytes = workspace_bytes_of(m, n, k);
+    *bytes = n > 0 && k > 0 ? way_of(m, n, k).parts_bytes(n, k) : 0;
     return LSGD_OK;
 }
 
@@ -507,7 +503,8 @@ LSGD_API lsgd_status lsgd_weight_grad8(const void* grad, const void* x, const vo
     LSGD_TRY(check_sizes(m, n, k));
     if (n == 0 || k == 0 || (m == 0 && accumulate)) return LSGD_OK;
     LSGD_TRY(check_buffer(out, 16, "out"));
-    const size_t need = workspace_bytes_of(m, n, k);
+    const Way w = way_of(m, n, k);
+    const size_t need = w.parts_bytes(n, k);
     if (m > 0) {
         LSGD_TRY(check_buffer(grad, 16, "grad"));
         LSGD_TRY(check_buffer(x, 16, "x"));
@@ -526,8 +523,8 @@ LSGD_API lsgd_status lsgd_weight_grad8(const void* grad, const void* x, const vo
         LSGD_TRY(ranges.check());
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return odt == LSGD_F32 ? launch<float>(grad, x, x_scales, m, n, k, out, accumulate != 0, workspace, s)
-                           : launch<uint16_t>(grad, x, x_scales, m, n, k, out, accumulate != 0, workspace, s);
+    return odt == LSGD_F32 ? launch<float>(w, grad, x, x_scales, m, n, k, out, accumulate != 0, workspace, s)
+                           : launch<uint16_t>(w, grad, x, x_scales, m, n, k, out, accumulate != 0, workspace, s);
 }
 
 }  // extern "C"
