@@ -127,29 +127,12 @@ __device__ __forceinline__ void load8(const uint16_t* p, int k, float (&x)[8]) {
     }
 }
 // The same for what is read once only: it does not stay in the caches.
-__device__ __forceinline__ void load8_once(const float* p, int k, float (&x)[8]) {
-    if (k < 8) return load8(p, k, x);
-    const f32x4_u a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p));
-    const f32x4_u b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_u*>(p + 4));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
-}
 __device__ __forceinline__ void load8_once(const uint16_t* p, int k, float (&x)[8]) {
     if (k < 8) return load8(p, k, x);
     const u32x4_u2 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_u2*>(p));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         x[2 * i] = bf16_to_f32(a[i] & 0xffffu), x[2 * i + 1] = __builtin_bit_cast(float, a[i] & 0xffff0000u);
-}
-__device__ __forceinline__ void store8(float* p, int k, const float (&x)[8]) {
-    if (k >= 8) {
-        *reinterpret_cast<f32x4_u*>(p) = f32x4_u{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4_u*>(p + 4) = f32x4_u{x[4], x[5], x[6], x[7]};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < k) p[i] = x[i];
-    }
 }
 __device__ __forceinline__ void store8(uint16_t* p, int k, const float (&x)[8]) {
     if (k >= 8) {

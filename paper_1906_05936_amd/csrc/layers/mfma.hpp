@@ -72,31 +72,6 @@ struct Buffer {
     }
 };
 
-// Shapes the instructions of a stretch of code between barriers: N times a
-// matrix instruction, an LDS read and two global loads, as far as there are any.
-template <int N>
-__device__ __forceinline__ void interleave_reads() {
-    unrolled<N>([](auto) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x20, 2, 0);
-    });
-}
-
-// The same for 16 matrix instructions: conversions and LDS writes between the first
-// half, so that the reads between the second do not wait behind them.
-__device__ __forceinline__ void interleave_writes() {
-    unrolled<8>([](auto) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
-        __builtin_amdgcn_sched_group_barrier(0x200, 2, 0);
-    });
-    unrolled<8>([](auto) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-    });
-}
-
 // The workgroup's loads into LDS issued so far have arrived, and all its waves
 // are past their earlier LDS accesses.
 __device__ __forceinline__ void loads_done() {
@@ -159,9 +134,6 @@ __device__ __forceinline__ f32x4 multiply(const Widened32& x, const Widened32& y
     for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.part[i], y.part[i], acc, 0, 0, 0);
     return acc;
 }
-
-__device__ __forceinline__ float value_of(float x) { return x; }
-__device__ __forceinline__ float value_of(uint16_t x) { return bf16_to_f32(x); }
 
 }  // namespace layers
 }  // namespace lsgd

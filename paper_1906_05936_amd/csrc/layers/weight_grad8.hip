@@ -22,7 +22,6 @@ __device__ __forceinline__ void put4(float* part, OT* out, int64_t at, int left,
 constexpr int kStep = 64;      // rows of grad and x a stage adds up
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 // 8 neighbours along the rows of the lane's column: the instruction hands each of 16
 // lanes four rows of its column.
