@@ -484,8 +484,9 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     // 11.7 / 15.0 / 40, 512x512x512 5.2 / 5.2 / 4.0 / 4.5 / 6.3 / 8.3, 256x2048x2048
     // 15.9 / 15.6 / 10.0 / 7.0 / 9.7 / 21, 1024x1024x4096 46 / 49 / 29 / 22 / 16 / 41
     // (about 4 of each is the call; to binary32 the same).
+    const int64_t cus = device_cus();
     const auto fits = [&](int64_t rows, int64_t cols) {
-        return ceil_div(a.rows, rows) * ceil_div(b.rows, cols) <= device_cus();
+        return ceil_div(a.rows, rows) * ceil_div(b.rows, cols) <= cus;
     };
     if (fits(16, 16)) return launch_narrow<1, 1, 8, 2, OT>(a, b, k, out, s);
     if (fits(32, 16)) return launch_narrow<2, 1, 8, 2, OT>(a, b, k, out, s);
@@ -494,7 +495,7 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     // Two rounds of 64 x 64 outputs are faster than one of 128 x 128 where many columns
     // are summed: us, 64 x 64 / 128 x 128: 1792x848x2804 23 / 28, 166x6658x2723 22 / 27,
     // 1402x951x1610 18 / 19, 794x1835x724 13 / 12.
-    const bool two_rounds = k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * device_cus();
+    const bool two_rounds = k > 2048 && ceil_div(a.rows, 64) * ceil_div(b.rows, 64) <= 2 * cus;
     if (fits(64, 64) || two_rounds) return launch_narrow<4, 4, 4, 2, OT>(a, b, k, out, s);
     // A round of 256 x 256 tiles takes about as long as one of two 128 x 128 tiles per
     // compute unit, which hold half of it: k = 4096, us to bfloat16, wide / 128 x 128:
@@ -503,8 +504,8 @@ lsgd_status launch(const Operand& a, const Operand& b, int64_t k, void* out, hip
     // 156 / 145, 157 / 176, 367 / 471).
     const TileOrder wide(ceil_div(a.rows, 256), ceil_div(b.rows, 256));
     const int64_t tiles = ceil_div(a.rows, 128) * ceil_div(b.rows, 128);
-    if (a.rows >= kWideTile && b.rows >= kWideTile && k > 128 && ceil_div(wide.tiles(), 256) < ceil_div(tiles, 512)) {
-        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), device_cus() / 8 * 8)));
+    if (a.rows >= kWideTile && b.rows >= kWideTile && k > 128 && ceil_div(wide.tiles(), cus) < ceil_div(tiles, 2 * cus)) {
+        const dim3 grid(static_cast<unsigned>(std::min<int64_t>(wide.blocks(), cus / 8 * 8)));
         hipLaunchKernelGGL((matmul8_wide_kernel<OT>), grid, dim3(256), 0, s, a, b, static_cast<uint32_t>(pitch8(k)),
                            static_cast<uint32_t>(scale_pitch8(k)), wide, static_cast<OT*>(out));
         return check_launch("lsgd_matmul8");
