@@ -91,7 +91,9 @@ __global__ __launch_bounds__(kBlock) void quant_rows_kernel(const T* __restrict_
 // into LDS as they are and transposed, from where every copy is written in rows
 // of 128 bytes. The transpose of each 4 x 4 happens in registers. Bound by the
 // parameters read and the copies written (8192 x 2048, four copies and four
-// transposed: 32 us, 6.3 TB/s; with stores through the caches 47), and where the
+// transposed: 32 us, 6.3 TB/s; with stores through the caches 47; one copy and one
+// transposed of 4096 x 4096, past the caches / through them: 22.2 / 23.4 us, with a product
+// of 16 rows behind it 29.2 / 29.4, of 512 rows 57 / 53), and where the
 // tiles are few by the way from load to store (1000 x 777: 4.9 us; with four 4 x 4 to
 // each of a quarter of the lanes 7.3, and 33 for the large one). Up to kCopies copies
 // a launch keep their pointers in the kernel's arguments; up to kLaunchTiles tiles
