@@ -180,6 +180,19 @@ def test_grad_of_a_table_whose_rows_take_every_digit(rows):
     assert torch.equal(out, want)
 
 
+def test_grad_of_the_most_entries():
+    """2^28 of them: four workers that hold the same tensors (whole numbers: exact)."""
+    n, rows = 1 << 26, 1003
+    tokens, g = zipf(n, rows + 5, 1, torch.int32), randint(n, -3, 4, seed=2).to(BF16).view(n, 1)
+    spread = tokens.long() * 512 + torch.arange(n, device=DEV) % 512   # 512 partial sums of a row
+    want = torch.zeros((rows + 5) * 512, device=DEV, dtype=torch.float64).index_add_(0, spread, g[:, 0].double())
+    want = want.view(rows + 5, 512).sum(1) * 4
+    assert want.abs().max() < 1 << 24
+    out = nans(rows, 1)
+    lsgd.embed_grad([g] * 4, [tokens] * 4, out, scale=0.5)
+    assert torch.equal(out[:, 0].double(), want[:rows] * 0.5)
+
+
 def test_grad_no_tokens():
     none = torch.empty(0, dtype=torch.int64, device=DEV)
     out = nans(5, 9)
