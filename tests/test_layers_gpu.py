@@ -473,6 +473,26 @@ def test_matmul8_small_terms_beside_large_ones_that_cancel(odt, m, n, k):
 
 
 @pytest.mark.parametrize("odt", [F32, BF16])
+@pytest.mark.parametrize("ablock,bblock", [(1, 128), (1, 1)])
+@pytest.mark.parametrize("m,n,k", [(3, 20, 300), (33, 1000, 777), (150, 1400, 2100), (600, 2100, 1300), (1200, 2100, 300), (2200, 4003, 900)])
+def test_matmul8_differences_of_large_sums(odt, ablock, bblock, m, n, k):
+    """Rows of b that repeat themselves with the other sign but for 2^-6 of their
+    size: nearly all of a sum cancels, and its rest has to be right to binary32's
+    roundings of the magnitudes, k * 2^-24, and the output's own."""
+    a, b = randn(m, k, seed=1), randn(n, k, seed=2)
+    half = k // 2
+    a[:, half:2 * half] = a[:, :half]
+    b[:, half:2 * half] = -b[:, :half] * (1 + 2.0 ** -6 * randn(n, half, seed=3))
+    (qa, sa), (qb, sb) = as8(a, ablock), as8(b, bblock)
+    va, vb = values(qa, sa, ablock, k), values(qb, sb, bblock, k)
+    want, size = va @ vb.t().contiguous(), va.abs() @ vb.abs().t().contiguous()
+    out = nans(m, n, dtype=odt)
+    lsgd.matmul8(qa, sa, qb, sb, out)
+    bound = size * (lsgd.pitch8(k) * U32)
+    assert_close(out, want, bound * 1.01 + want.abs() * HALF[BF16] if odt == BF16 else bound)
+
+
+@pytest.mark.parametrize("odt", [F32, BF16])
 def test_matmul8_scales_at_their_ends(odt):
     """Elements near 2^100 against elements near 2^-100: the scales meet in
     binary32's range though neither lies near 1."""
